@@ -24,7 +24,7 @@
  *     device pointer, `st_read_tensor`) wait for the stream.
  *   - Errors are status codes; nothing aborts, throws or traps.  `st_last_error` gives a
  *     text for the most recent failure on that context (or, with NULL, of the last failed
- *     `st_init_head` on this thread).  All shapes are validated on the host before any
+ *     `st_init_head`, `st_adamw_create`, `st_quantize_rows` or `st_int8_matmul` on this thread).  All shapes are validated on the host before any
  *     kernel is launched.
  *   - A context is bound to the device that was current in `st_init_head`, and must be
  *     used from one host thread at a time.
@@ -346,6 +346,110 @@ ST_API st_status st_measure_arithmetic_peaks(void *cuda_stream, double *fma_tflo
 ST_API st_status st_agreement_noalloc(const uint8_t *pred, const uint8_t *label, int64_t n_pixels,
                                       int32_t n_classes, void *cuda_stream, int64_t *conf_out,
                                       double *miou_out);
+
+/* ---- operators around the step: the optimiser of tensors that no context holds ------------------------- */
+
+/* Element types of tensors that are not fp32 by definition. */
+typedef enum st_dtype { ST_F32 = 0, ST_BF16 = 1, ST_F16 = 2 } st_dtype;
+
+/*
+ * st_adamw — OptimStep (Algorithm 1, Section 5.2: Adam) for any number of tensors at once, with decoupled weight decay.
+ * A context trains the head that it holds; this trains what lies outside of it: every layer of the student in full distillation
+ * (Section 5.3's comparison) or in its pre-training (Section 5.2), or a teacher that is fine-tuned.  Step t = 1, 2, ... on each
+ * value p with gradient g, moments m and v:
+ *     g <- f g
+ *     m <- beta1 m + (1 - beta1) g
+ *     v <- beta2 v + (1 - beta2) g^2
+ *     p <- p - lr wd p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * lr and wd of a tensor are the optimiser's lr times the tensor's lr_scale, and the tensor's weight_decay.  f is grad_scale of the
+ * call, times min(1, max_norm / (norm + 1e-6)) with max_norm > 0; norm is the Euclidean norm of all gradients together, grad_scale
+ * included, summed in double in an order that depends on the tensors' sizes alone.
+ *
+ * Moments in 32 bits are fp32 [n] each.  Moments in 8 bits are one byte a value, in blocks of ST_ADAMW_BLOCK consecutive values of a
+ * tensor (its last block may be shorter) with one fp32 scale each:
+ *     m = c |c| scale, c = -127..127 in int8;     sqrt(v) = c^2 scale, c = 0..255 in uint8
+ * where scale is the block's largest |m| / 127^2 (0, with all c = 0, if that |m| is below 2^-100) or its largest sqrt(v) / 255^2.
+ * c is the level whose root is nearest: floor(sqrt(|m| / scale) + 1/2); a value with v > 0 has c >= 1, so that no step divides
+ * by a second moment that was rounded to nothing.  The levels lie closer together near zero: between 1e-4 of the block's largest
+ * value and that value itself they are 1.6 to 16 per cent apart (m; v about half of that in its root).  The step works with the moments in fp32
+ * (with 8 bits: each product and sum rounded by itself, so that equal inputs give equal levels) and parameters see them before they
+ * are rounded to levels.  A block that holds a moment that is not finite decodes to values that are not finite or NaN.
+ */
+#define ST_ADAMW_BLOCK 256
+typedef struct st_adamw st_adamw; /* opaque, library-owned */
+
+typedef struct st_adamw_tensor {
+    void *param;               /* device; [n] of param_type, updated in place */
+    float *master;             /* device; NULL, or fp32 [n]: the values the step works on, `param` is then their rounded copy and not read */
+    const void *grad;          /* device; [n] of grad_type, or NULL: the tensor is left alone (see st_adamw_set_grads) */
+    void *exp_avg;             /* device; m: fp32 [n], or int8 [n] */
+    void *exp_avg_sq;          /* device; v: fp32 [n], or uint8 [n] */
+    float *exp_avg_scale;      /* device; with 8-bit moments fp32 [ceil(n / ST_ADAMW_BLOCK)], else not used */
+    float *exp_avg_sq_scale;
+    int64_t n;                 /* values; 0 is a tensor without any */
+    int32_t param_type;        /* st_dtype */
+    int32_t grad_type;
+    float weight_decay;
+    float lr_scale;
+} st_adamw_tensor;
+
+typedef struct st_adamw_desc {
+    int32_t n_tensors;         /* 1..65535 */
+    int32_t state_bits;        /* 32 or 8 */
+    double lr;                 /* >= 0 */
+    double beta1, beta2;       /* in [0, 1) */
+    double eps;                /* at least FLT_MIN */
+    double max_norm;           /* 0: gradients are not clipped */
+    int32_t skip_nonfinite;    /* 1: where the gradients' norm is not finite nothing is changed and the step is not counted */
+    int64_t first_step;        /* steps taken before (a resumed training); 0 at the beginning */
+    void *cuda_stream;         /* cudaStream_t on which all work of this optimiser is enqueued (NULL = default stream) */
+} st_adamw_desc;
+
+/*
+ * st_adamw_create — an optimiser over `tensors` (host array of desc->n_tensors, copied).
+ * All buffers stay the caller's and must stay where they are as long as the optimiser is used: it works on them in place and holds
+ * nothing but the step count, the learning rate and a table of the pointers.  A new training starts from moments (and scales) of zero.
+ * Buffers may start at any multiple of their element's size; those that start at multiples of 16 bytes (8-bit moments: of 4)
+ * take the faster path.
+ * ST_ERR_INVALID_ARG: a NULL or inconsistent description; a pointer that is not memory of the current device or not aligned to its
+ * element; two buffers that are written overlapping, or a gradient overlapping one that is written.  ST_ERR_UNSUPPORTED: more than
+ * 2^42 values.
+ */
+ST_API st_status st_adamw_create(const st_adamw_desc *desc, const st_adamw_tensor *tensors, st_adamw **out);
+
+/*
+ * st_adamw_set_grads — where the gradients are from now on: for steps enqueued after this call, and for steps of a captured graph
+ * that are replayed after it (a graph that holds this call sets them again when it is replayed).
+ *   grads   host array of n_tensors device pointers; NULL entries leave their tensors alone (no decay either).
+ * A caller whose gradients keep their buffers gives them to st_adamw_create and never calls this.
+ */
+ST_API st_status st_adamw_set_grads(st_adamw *opt, const void *const *grads);
+
+/* The learning rate of steps enqueued after this call, and of replayed ones (as above).  Not part of the tensors' lr_scale. */
+ST_API st_status st_adamw_set_lr(st_adamw *opt, double lr);
+
+/*
+ * st_adamw_step — one step on all tensors: one kernel, and one more in front of it that measures the gradients' norm where max_norm,
+ * skip_nonfinite or norm_out asks for it.  Returns at once; may be captured into a graph.
+ *   grad_scale  finite; multiplies every gradient (1 / the loss scale of fp16 training).
+ *   norm_out    device, or NULL; one fp32: the norm before clipping.
+ */
+ST_API st_status st_adamw_step(st_adamw *opt, float grad_scale, float *norm_out);
+
+/*
+ * st_adamw_read_moments / st_adamw_write_moments — the moments as fp32 values, whatever they are held in: what a checkpoint keeps, and
+ * how it moves between 8 and 32 bits.  Work is enqueued on the optimiser's stream.
+ *   exp_avg, exp_avg_sq   host arrays of n_tensors device pointers to fp32 [n] each; a NULL entry leaves that tensor's moment out, a
+ *                         NULL array all of them.  Reading: the buffers must not overlap the optimiser's own.
+ * Written into 8 bits, values are rounded to levels as a step does.  Negative second moments are taken as 0.
+ */
+ST_API st_status st_adamw_read_moments(st_adamw *opt, float *const *exp_avg, float *const *exp_avg_sq);
+ST_API st_status st_adamw_write_moments(st_adamw *opt, const float *const *exp_avg, const float *const *exp_avg_sq);
+
+/* Steps taken so far, first_step included (host; waits for the stream: a skipped step is not counted). */
+ST_API st_status st_adamw_step_count(st_adamw *opt, int64_t *steps);
+ST_API void st_adamw_destroy(st_adamw *opt);
+ST_API const char *st_adamw_last_error(const st_adamw *opt);
 
 /* ---- host-side pieces around the step: no device work, callable without a GPU ------------------------ */
 

@@ -43,9 +43,15 @@ EXPORTED = [
     "st_agreement_noalloc", "st_train_key_frame", "st_next_stride", "st_client_schedule", "st_throughput_bounds",
     "st_traffic_bounds", "st_choose_max_updates", "st_apply_update", "st_measure_arithmetic_peaks",
     "st_prefetch_key_frame", "st_use_prefetched_key_frame", "st_head_param_counts", "st_set_skip_features",
+    "st_adamw_create", "st_adamw_set_grads", "st_adamw_set_lr", "st_adamw_step", "st_adamw_read_moments",
+    "st_adamw_write_moments", "st_adamw_step_count", "st_adamw_destroy", "st_adamw_last_error",
 ]
 ST_NOALLOC_MAX_CLASSES = 64
 ST_MAX_STAGES = 12
+ST_F32 = 0
+ST_BF16 = 1
+ST_F16 = 2
+ST_ADAMW_BLOCK = 256
 
 
 class st_head_desc(ctypes.Structure):
@@ -59,6 +65,23 @@ class st_head_desc(ctypes.Structure):
         ("background_class", ctypes.c_int32),
         ("n_blocks", ctypes.c_int32), ("block_c_out", ctypes.c_int32 * 2), ("block_c_skip", ctypes.c_int32 * 2),
         ("first_trained", ctypes.c_int32),
+    ]
+
+
+class st_adamw_tensor(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+        ("exp_avg_sq", ctypes.c_void_p), ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p),
+        ("n", ctypes.c_int64), ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float),
+    ]
+
+
+class st_adamw_desc(ctypes.Structure):
+    _fields_ = [
+        ("n_tensors", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("max_norm", ctypes.c_double), ("skip_nonfinite", ctypes.c_int32),
+        ("first_step", ctypes.c_int64), ("cuda_stream", ctypes.c_void_p),
     ]
 
 
@@ -132,6 +155,24 @@ def load_library() -> ctypes.CDLL:
     lib.st_agreement_noalloc.argtypes = [vp, vp, i64, i32, vp, vp, vp]
     lib.st_measure_arithmetic_peaks.restype = ctypes.c_int
     lib.st_measure_arithmetic_peaks.argtypes = [vp, ctypes.POINTER(dbl), ctypes.POINTER(dbl)]
+    lib.st_adamw_create.restype = ctypes.c_int
+    lib.st_adamw_create.argtypes = [ctypes.POINTER(st_adamw_desc), ctypes.POINTER(st_adamw_tensor), ctypes.POINTER(vp)]
+    lib.st_adamw_set_grads.restype = ctypes.c_int
+    lib.st_adamw_set_grads.argtypes = [vp, vp]
+    lib.st_adamw_set_lr.restype = ctypes.c_int
+    lib.st_adamw_set_lr.argtypes = [vp, dbl]
+    lib.st_adamw_step.restype = ctypes.c_int
+    lib.st_adamw_step.argtypes = [vp, ctypes.c_float, vp]
+    lib.st_adamw_read_moments.restype = ctypes.c_int
+    lib.st_adamw_read_moments.argtypes = [vp, vp, vp]
+    lib.st_adamw_write_moments.restype = ctypes.c_int
+    lib.st_adamw_write_moments.argtypes = [vp, vp, vp]
+    lib.st_adamw_step_count.restype = ctypes.c_int
+    lib.st_adamw_step_count.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.st_adamw_destroy.restype = None
+    lib.st_adamw_destroy.argtypes = [vp]
+    lib.st_adamw_last_error.restype = ctypes.c_char_p
+    lib.st_adamw_last_error.argtypes = [vp]
     lib.st_launch_count.restype = i64
     lib.st_launch_count.argtypes = [vp]
     lib.st_destroy.restype = None
@@ -145,7 +186,9 @@ def load_library() -> ctypes.CDLL:
 
 
 # ---------------------------------------------------------------------------- marshalling
-_NP_OF = {"float32": np.float32, "float64": np.float64, "uint8": np.uint8, "int32": np.int32, "int64": np.int64}
+_NP_OF = {"float32": np.float32, "float64": np.float64, "uint8": np.uint8, "int8": np.int8, "int32": np.int32, "int64": np.int64,
+          "float16": np.float16}
+_TYPE_OF = {"float32": ST_F32, "bfloat16": ST_BF16, "float16": ST_F16}       # st_dtype of a tensor's element type
 _NAME_OF = {}        # torch dtype object -> its name here, filled as they are met (a look-up per call instead of a string)
 
 
@@ -154,7 +197,7 @@ def _ptr(buf, dtype: str, min_elems: int, what: str) -> Optional[int]:
     if buf is None:
         return None
     if isinstance(buf, np.ndarray):
-        if buf.dtype != _NP_OF[dtype] or not buf.flags.c_contiguous:
+        if buf.dtype != _NP_OF.get(dtype) or not buf.flags.c_contiguous:
             raise TypeError(f"{what}: need a C-contiguous {dtype} array, got {buf.dtype}")
         if buf.size < min_elems:
             raise ValueError(f"{what}: {buf.size} elements, need {min_elems}")
@@ -375,6 +418,136 @@ def st_measure_arithmetic_peaks(cuda_stream: int = 0):
     _status_only(load_library().st_measure_arithmetic_peaks(cuda_stream or None, ctypes.byref(fma), ctypes.byref(ex2)),
                  "st_measure_arithmetic_peaks")
     return fma.value, ex2.value
+
+
+# ---------------------------------------------------------------------------- the optimiser of tensors outside a context
+class _AdamW:
+    """Handle of an st_adamw, with the tensors that it works on (they must outlive it)."""
+
+    def __init__(self, handle, sizes, grad_names, keep):
+        self.handle = handle
+        self.sizes = sizes
+        self.grad_names = grad_names
+        self.keep = keep
+        self.grads = None
+
+    def __del__(self):
+        try:
+            st_adamw_destroy(self)
+        except Exception:
+            pass
+
+
+def _check_adamw(status: int, opt: Optional[_AdamW]) -> None:
+    if status == ST_OK:
+        return
+    lib = load_library()
+    msg = lib.st_adamw_last_error(opt.handle if opt is not None else None)
+    raise StError(status, lib.st_status_name(status).decode(), (msg or b"").decode())
+
+
+def _dtype_name(t, what: str) -> str:
+    name = str(t.dtype).removeprefix("torch.")
+    if name not in _TYPE_OF:
+        raise TypeError(f"{what}: need float32, bfloat16 or float16, got {t.dtype}")
+    return name
+
+
+def _pointers(tensors, sizes, names, what: str):
+    """Array of the tensors' addresses (a None among them is NULL); None for None."""
+    if tensors is None:
+        return None
+    if len(tensors) != len(sizes):
+        raise ValueError(f"{what}: {len(tensors)} tensors, need {len(sizes)}")
+    return (ctypes.c_void_p * len(sizes))(*[_ptr(t, name, n, what) for t, n, name in zip(tensors, sizes, names)])
+
+
+def st_adamw_create(params, exp_avg, exp_avg_sq, grads=None, exp_avg_scale=None, exp_avg_sq_scale=None, masters=None, *,
+                    lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay=0.01, lr_scale=1.0,
+                    max_norm: float = 0.0, skip_nonfinite: bool = False, first_step: int = 0, grad_types=None,
+                    cuda_stream: int = 0) -> _AdamW:
+    """Lists of CUDA tensors, one entry per parameter tensor.  `params` float32, bfloat16 or float16; `exp_avg` and `exp_avg_sq`
+    float32, or int8 and uint8 with `exp_avg_scale` and `exp_avg_sq_scale` (float32, one value per ST_ADAMW_BLOCK values);
+    `grads` and `masters` may hold None.  `weight_decay` and `lr_scale`: a number or one per tensor.  `grad_types`: names of the
+    gradients' types ("float32", "bfloat16", "float16"), one or one per tensor, where `grads` does not say (default: the parameter's)."""
+    count = len(params)
+    sizes = [p.numel() for p in params]
+    eight = count > 0 and str(exp_avg[0].dtype).removeprefix("torch.") == "int8"
+    if eight and (exp_avg_scale is None or exp_avg_sq_scale is None):
+        raise ValueError("8-bit moments need exp_avg_scale and exp_avg_sq_scale")
+
+    def each(value):
+        return list(value) if hasattr(value, "__len__") and not isinstance(value, str) else [value] * count
+
+    grads = grads if grads is not None else [None] * count
+    masters = masters if masters is not None else [None] * count
+    scales = exp_avg_scale if eight else [None] * count, exp_avg_sq_scale if eight else [None] * count
+    decay, lr_scales, types = each(weight_decay), each(lr_scale), each(grad_types)
+    for name, value in (("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq), ("grads", grads), ("masters", masters), ("exp_avg_scale", scales[0]),
+                        ("exp_avg_sq_scale", scales[1]), ("weight_decay", decay), ("lr_scale", lr_scales), ("grad_types", types)):
+        if len(value) != count:
+            raise ValueError(f"{name}: {len(value)} entries, need {count}")
+    table, grad_names = (st_adamw_tensor * max(count, 1))(), []
+    for i, p in enumerate(params):
+        n, name = sizes[i], _dtype_name(p, "params")
+        blocks = -(-n // ST_ADAMW_BLOCK)
+        grad_name = _dtype_name(grads[i], "grads") if grads[i] is not None else types[i] if types[i] is not None else name
+        grad_names.append(grad_name)
+        table[i] = st_adamw_tensor(
+            _ptr(p, name, n, "params"), _ptr(masters[i], "float32", n, "masters"), _ptr(grads[i], grad_name, n, "grads"),
+            _ptr(exp_avg[i], "int8" if eight else "float32", n, "exp_avg"), _ptr(exp_avg_sq[i], "uint8" if eight else "float32", n, "exp_avg_sq"),
+            _ptr(scales[0][i], "float32", blocks, "exp_avg_scale"), _ptr(scales[1][i], "float32", blocks, "exp_avg_sq_scale"),
+            n, _TYPE_OF[name], _TYPE_OF[grad_name], decay[i], lr_scales[i])
+    desc = st_adamw_desc(count, 8 if eight else 32, lr, beta1, beta2, eps, max_norm, int(skip_nonfinite), first_step, cuda_stream or None)
+    out = ctypes.c_void_p()
+    _check_adamw(load_library().st_adamw_create(ctypes.byref(desc), table, ctypes.byref(out)), None)
+    opt = _AdamW(out.value, sizes, grad_names, (list(params), list(exp_avg), list(exp_avg_sq), scales, list(masters)))
+    opt.grads = list(grads)
+    return opt
+
+
+def st_adamw_set_grads(opt: _AdamW, grads) -> None:
+    """Where the gradients are from now on (None: leave that tensor alone); the tensors must outlive the steps that read them."""
+    _check_adamw(load_library().st_adamw_set_grads(opt.handle, _pointers(grads, opt.sizes, opt.grad_names, "grads")), opt)
+    opt.grads = list(grads)
+
+
+def st_adamw_set_lr(opt: _AdamW, lr: float) -> None:
+    _check_adamw(load_library().st_adamw_set_lr(opt.handle, lr), opt)
+
+
+def st_adamw_step(opt: _AdamW, grad_scale: float = 1.0, norm_out=None) -> None:
+    """One step on all tensors; `norm_out` (CUDA float32, one element) receives the gradients' norm before clipping."""
+    _check_adamw(load_library().st_adamw_step(opt.handle, grad_scale, _ptr(norm_out, "float32", 1, "norm_out")), opt)
+
+
+def st_adamw_read_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
+    """The moments as float32 values into lists of CUDA tensors (an entry or a list may be None)."""
+    names = ["float32"] * len(opt.sizes)
+    _check_adamw(load_library().st_adamw_read_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
+                                                      _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
+
+
+def st_adamw_write_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
+    names = ["float32"] * len(opt.sizes)
+    _check_adamw(load_library().st_adamw_write_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
+                                                       _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
+
+
+def st_adamw_step_count(opt: _AdamW) -> int:
+    steps = ctypes.c_int64(0)
+    _check_adamw(load_library().st_adamw_step_count(opt.handle, ctypes.byref(steps)), opt)
+    return int(steps.value)
+
+
+def st_adamw_destroy(opt: Optional[_AdamW]) -> None:
+    if opt is not None and opt.handle:
+        load_library().st_adamw_destroy(opt.handle)
+        opt.handle = None
+
+
+def st_adamw_last_error(opt: Optional[_AdamW]) -> str:
+    return (load_library().st_adamw_last_error(opt.handle if opt else None) or b"").decode()
 
 
 class st_latencies(ctypes.Structure):

@@ -128,6 +128,21 @@ st_status fail(st_ctx* ctx, st_status code, const char* fmt, ...)
     return code;
 }
 
+}  // namespace
+
+int st::fail_on_thread(int code, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    g_init_error = buf;
+    return code;
+}
+
+namespace {
+
 #define ST_CUDA(ctx, call)                                                                        \
     do {                                                                                          \
         cudaError_t e_ = (call);                                                                  \

@@ -75,6 +75,9 @@ inline size_t one_per_sm(size_t smem, int64_t blocks, int n_sms)
 }
 #endif
 
+// The text that st_last_error(NULL) gives on this thread, from a printf format; returns `code` (an st_status)
+int fail_on_thread(int code, const char* fmt, ...);
+
 constexpr int kUp = 4;            // bilinear upsample factor of the head (frame = feature map * 4)
 constexpr int kMaxSteps = 64;     // upper bound of n_steps in one st_distill_step call
 constexpr int kClassPad = 32;     // class rows of bf16 GEMM operands are padded to this (UMMA N)
