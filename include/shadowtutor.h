@@ -409,8 +409,8 @@ typedef struct st_adamw_desc {
  * st_adamw_create — an optimiser over `tensors` (host array of desc->n_tensors, copied).
  * All buffers stay the caller's and must stay where they are as long as the optimiser is used: it works on them in place and holds
  * nothing but the step count, the learning rate and a table of the pointers.  A new training starts from moments (and scales) of zero.
- * Buffers may start at any multiple of their element's size; those that start at multiples of 16 bytes (8-bit moments: of 4)
- * take the faster path.
+ * Buffers may start at any multiple of their element's size; those that start at multiples of eight
+ * elements take the faster path.
  * ST_ERR_INVALID_ARG: a NULL or inconsistent description; a pointer that is not memory of the current device or not aligned to its
  * element; two buffers that are written overlapping, or a gradient overlapping one that is written.  ST_ERR_UNSUPPORTED: more than
  * 2^42 values.

@@ -1,14 +1,13 @@
 // st_adamw — OptimStep of Algorithm 1 (Adam, Section 5.2; here with decoupled weight decay) over any number of the caller's
 // tensors in one launch, moments in fp32 or in 8 bits.  The formulas stand in include/shadowtutor.h.
 //
-// All tensors are cut into chunks of kChunk values; a table on the device says which tensor a chunk belongs to, and the blocks of a
-// launch that fills the GPU once walk over it.  A warp takes 256 consecutive values of a chunk, which are also a block of 8-bit
+// All tensors are cut into chunks of kChunk values; a table on the device says which tensor a chunk belongs to, and each block of a
+// launch that fills the GPU once takes an equal part of them.  A warp takes 256 consecutive values of a chunk, which are also a block of 8-bit
 // moments: the two maxima that a block's scales need are warp reductions, and a lane keeps its eight values in registers from the
 // load to the store, so that every buffer is read once and written once.
 //
 // The gradients' norm needs every gradient before the first step is taken: a kernel of its own (double accumulators, partial
-// sums per block added in block order: the result depends on nothing but the values and the launch).  The step then walks the
-// chunks from the last to the first, so that it begins with the gradients that the norm has just left in L2.
+// sums per block added in block order: the result depends on nothing but the values and the launch).
 #include "../../include/shadowtutor.h"
 #include "st_internal.h"
 
@@ -21,6 +20,7 @@
 #include <cstdio>
 #include <new>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 namespace st {
@@ -30,10 +30,10 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kBlockVals = ST_ADAMW_BLOCK;                  // one warp's values: a block of 8-bit moments
 constexpr int kChunk = kWarps * kBlockVals;
 constexpr int kPer = kBlockVals / 32;                       // values of a lane
-static_assert(kPer == 8, "the vector path below moves two groups of four values per lane");
+static_assert(kPer == 8, "the vector path below moves eight values per lane");
 
-struct TensorRec {
-    void* param; float* master; const void* grad;
+struct TensorRec {              // does not change as long as the optimiser lives (the gradients' addresses may: Plan::grads)
+    void* param; float* master;
     void *m, *v; float *m_scale, *v_scale;
     int64_t n;
     float wd, lr_scale;
@@ -43,38 +43,38 @@ struct ChunkRec { int32_t tensor, index; };
 struct Scalars {
     long long t;                // steps taken
     double lr;
+    float bias[2][2];           // of step t at [t % 2]: 1 / (1 - beta1^t) and 1 / sqrt(1 - beta2^t)
     float factor;               // of the gradients, from the norm
     int skip;                   // the norm is not finite and the step is to be left out
     unsigned int norm_ticket, step_ticket;
 };
 struct Plan {
-    TensorRec* tensors; const ChunkRec* chunks; int64_t n_chunks;
+    const TensorRec* tensors; const ChunkRec* chunks; int64_t n_chunks;
+    const void** grads;
     Scalars* sc; double* partials;
     double ln_b1, ln_b2, max_norm;
-    float b1, b2, omb1, omb2, eps;
+    float b1, b2, omb1, omb2, eps, one;
     int skip_nonfinite;
 };
 
 // ---- moving a warp's 256 values -------------------------------------------------------------------------
-// Vector path: lane l has values 4 l .. 4 l + 3 of each half of 128.  Otherwise (a block that a tensor's end cuts, or buffers
-// that lie unaligned): values l, 32 + l, ..., which moves whole sectors too, with four times the instructions.
+// Vector path: lane l has values 8 l .. 8 l + 7, one access per buffer (32 bytes of fp32, 16 of 16-bit values, 8 of codes).  Otherwise (a
+// block that a tensor's end cuts, or buffers that lie unaligned): values l, 32 + l, ..., which moves whole sectors too, with
+// eight times the accesses.
+__device__ __forceinline__ void load_256(uint32_t* r, const void* src)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(src) : "memory");
+}
 struct Raw { uint32_t w[kPer]; };
 template <bool VEC>
 __device__ __forceinline__ void fetch(Raw& r, const void* base, int type, int64_t at, int count, int lane)
 {
     if (VEC) {
-        if (type == ST_F32) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint4 q = *(const uint4*)((const float*)base + at + u * 128 + 4 * lane);
-                r.w[4 * u] = q.x; r.w[4 * u + 1] = q.y; r.w[4 * u + 2] = q.z; r.w[4 * u + 3] = q.w;
-            }
-        } else {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint2 q = *(const uint2*)((const uint16_t*)base + at + u * 128 + 4 * lane);
-                r.w[4 * u] = q.x; r.w[4 * u + 1] = q.y;
-            }
+        if (type == ST_F32) load_256(r.w, (const float*)base + at + kPer * lane);
+        else {
+            const uint4 q = *(const uint4*)((const uint16_t*)base + at + kPer * lane);
+            r.w[0] = q.x; r.w[1] = q.y; r.w[2] = q.z; r.w[3] = q.w;
         }
     } else {
 #pragma unroll
@@ -97,7 +97,7 @@ __device__ __forceinline__ void convert(float (&x)[kPer], const Raw& r, int type
     } else {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            const uint32_t h = VEC ? (r.w[(j & 4) + ((j & 3) >> 1)] >> ((j & 1) * 16)) & 0xffffu : r.w[j];
+            const uint32_t h = VEC ? (r.w[j >> 1] >> ((j & 1) * 16)) & 0xffffu : r.w[j];
             x[j] = from16(h, type);
         }
     }
@@ -106,15 +106,22 @@ __device__ __forceinline__ uint32_t to16(float x, int type)
 {
     return type == ST_BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x)) : (uint32_t)__half_as_ushort(__float2half_rn(x));
 }
+__device__ __forceinline__ uint32_t pair16(float lo, float hi, int type)
+{
+    if (type == ST_BF16) { const __nv_bfloat162 q = __floats2bfloat162_rn(lo, hi); return *(const uint32_t*)&q; }
+    const __half2 q = __floats2half2_rn(lo, hi);
+    return *(const uint32_t*)&q;
+}
 template <bool VEC>
 __device__ __forceinline__ void put(const float (&x)[kPer], void* base, int type, int64_t at, int count, int lane)
 {
     if (VEC) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float* y = x + 4 * u;
-            if (type == ST_F32) *(float4*)((float*)base + at + u * 128 + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
-            else *(uint2*)((uint16_t*)base + at + u * 128 + 4 * lane) = make_uint2(to16(y[0], type) | to16(y[1], type) << 16, to16(y[2], type) | to16(y[3], type) << 16);
+        if (type == ST_F32) {
+            const uint32_t r[kPer] = {__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]),
+                                      __float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
+            store_256((float*)base + at + kPer * lane, r);
+        } else {
+            *(uint4*)((uint16_t*)base + at + kPer * lane) = make_uint4(pair16(x[0], x[1], type), pair16(x[2], x[3], type), pair16(x[4], x[5], type), pair16(x[6], x[7], type));
         }
     } else {
 #pragma unroll
@@ -131,24 +138,28 @@ __device__ __forceinline__ void fetch_codes(Raw& r, const void* base, int64_t at
 {
     const uint8_t* b = (const uint8_t*)base + at;
     if (VEC) {
-        r.w[0] = *(const uint32_t*)(b + 4 * lane);
-        r.w[4] = *(const uint32_t*)(b + 128 + 4 * lane);
+        const uint2 q = *(const uint2*)(b + kPer * lane);
+        r.w[0] = q.x; r.w[4] = q.y;
     } else {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) { const int i = 32 * j + lane; r.w[j] = i < count ? b[i] : 0u; }
     }
 }
-template <bool VEC> __device__ __forceinline__ uint32_t code(const Raw& r, int j) { return VEC ? (r.w[j & 4] >> (8 * (j & 3))) & 0xffu : r.w[j]; }
+// Code j of a lane as fp32: its byte becomes the low byte of 2^23's mantissa (one permutation and one sum, where a conversion of an
+// integer goes through a slower unit).  `flip` and `base`: 0x80 in each byte and 2^23 + 128 for signed codes, 0 and 2^23 for others.
+template <bool VEC> __device__ __forceinline__ float code(const Raw& r, int j, uint32_t flip, float base)
+{
+    return VEC ? __uint_as_float(__byte_perm(r.w[j & 4] ^ flip, 0x4b000000u, 0x7440u | (j & 3))) - base
+               : __uint_as_float(__byte_perm(r.w[j] ^ flip, 0x4b000000u, 0x7440u)) - base;
+}
+__device__ __forceinline__ uint32_t low_bytes(const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0040u), __byte_perm(c[2], c[3], 0x0040u), 0x5410u); }
+// Codes come as the low bytes of 32-bit words
 template <bool VEC>
-__device__ __forceinline__ void put_codes(const int (&c)[kPer], void* base, int64_t at, int count, int lane)
+__device__ __forceinline__ void put_codes(const uint32_t (&c)[kPer], void* base, int64_t at, int count, int lane)
 {
     uint8_t* b = (uint8_t*)base + at;
     if (VEC) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int* q = c + 4 * u;
-            *(uint32_t*)(b + u * 128 + 4 * lane) = (q[0] & 0xff) | (q[1] & 0xff) << 8 | (q[2] & 0xff) << 16 | (uint32_t)q[3] << 24;
-        }
+        *(uint2*)(b + kPer * lane) = make_uint2(low_bytes(c), low_bytes(c + 4));
     } else {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) { const int i = 32 * j + lane; if (i < count) b[i] = (uint8_t)c[j]; }
@@ -163,26 +174,33 @@ __device__ __forceinline__ void decode(float (&m)[kPer], float (&root)[kPer], co
 {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int c = (int)(int8_t)code<VEC>(rm, j), d = (int)code<VEC>(rv, j);
-        m[j] = __fmul_rn((float)(c * abs(c)), m_scale);
-        root[j] = __fmul_rn((float)(d * d), v_scale);
+        const float c = code<VEC>(rm, j, 0x80808080u, 8388608.f + 128.f), d = code<VEC>(rv, j, 0u, 8388608.f);
+        m[j] = __fmul_rn(__fmul_rn(c, fabsf(c)), m_scale);
+        root[j] = __fmul_rn(__fmul_rn(d, d), v_scale);
     }
 }
 
-// floor(sqrt(r) + 1/2), at most `most`.  The approximate root is within 2^-22 of the root; where that can matter the two borders next
-// to the level, which fp32 holds exactly, decide.
-__device__ __forceinline__ int nearest_level(float r, int most)
+// The level floor(sqrt(r) + 1/2).  The approximate root lies within 2^-23 of the root (relative; 3e-5 of a level at level 255,
+// and as much again where `r` comes from an approximate root), so rounding it to the nearest whole number gives the level unless it lies as near as kNear to a border; there the border, which fp32 holds
+// exactly, decides.  One in 5000 values does: a lane that has met one among its sixteen takes that path for all of them.
+constexpr float kNear = 1e-4f, kRound = 12582912.f;         // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
+__device__ __forceinline__ float approximate_root(float r)
 {
     float s;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(s) : "f"(r));
-    float c = floorf(s + 0.5f);
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(r));
+    return s;
+}
+__device__ __forceinline__ float exact_level(float r)
+{
+    float c = floorf(approximate_root(r) + 0.5f);
     const float below = c - 0.5f, above = c + 0.5f;
     if (r < below * below && c > 0.f) c -= 1.f;
     if (r >= above * above) c += 1.f;
-    return min(__float2int_rz(c), most);        // NaN (a block that is not finite): 0
+    return c;
 }
-// Levels of a warp's block from m and sqrt(v), and its two scales
-__device__ __forceinline__ void encode(const float (&m)[kPer], const float (&root)[kPer], int (&cm)[kPer], int (&cv)[kPer], float& m_scale, float& v_scale)
+// Levels (low bytes) of a warp's block from m and sqrt(v), and its two scales.  No level leaves its range: the largest ratio is 127^2 or 255^2
+// to within 2^-22.
+__device__ __forceinline__ void encode(const float (&m)[kPer], const float (&root)[kPer], uint32_t (&cm)[kPer], uint32_t (&cv)[kPer], float& m_scale, float& v_scale)
 {
     uint32_t top = 0, top_root = 0;             // of values that are not negative the bits are in the values' order, and NaN is above infinity
 #pragma unroll
@@ -194,27 +212,70 @@ __device__ __forceinline__ void encode(const float (&m)[kPer], const float (&roo
     m_scale = a < 0x1p-100f ? 0.f : __fdiv_rn(a, 127.f * 127.f);
     v_scale = __fdiv_rn(b, 255.f * 255.f);
     const float im = m_scale > 0.f ? __frcp_rn(m_scale) : 0.f, iv = v_scale > 0.f ? __frcp_rn(v_scale) : 0.f;
+    float far = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int c = nearest_level(__fmul_rn(fabsf(m[j]), im), 127);
-        cm[j] = m[j] < 0.f ? -c : c;
-        const int d = nearest_level(__fmul_rn(root[j], iv), 255);
-        cv[j] = root[j] > 0.f ? max(d, 1) : d;
+        const float s = copysignf(approximate_root(__fmul_rn(fabsf(m[j]), im)), m[j]), y = s + kRound;
+        // a second moment that is not 0 has level 1 at least (the least root is 3.7e-23)
+        const float r = fmaxf(approximate_root(__fmul_rn(root[j], iv)), __saturatef(root[j] * FLT_MAX)), z = r + kRound;
+        far = fmaxf(far, fmaxf(fabsf(s - (y - kRound)), fabsf(r - (z - kRound))));
+        cm[j] = __float_as_uint(y);
+        cv[j] = __float_as_uint(z);
+    }
+    if (far > 0.5f - kNear) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const float c = exact_level(__fmul_rn(fabsf(m[j]), im)), d = exact_level(__fmul_rn(root[j], iv));
+            cm[j] = __float_as_uint(copysignf(c, m[j]) + kRound);
+            cv[j] = __float_as_uint(fmaxf(d, __saturatef(root[j] * FLT_MAX)) + kRound);
+        }
+    }
+}
+
+// ---- which values are a block's ---------------------------------------------------------------------------------
+// Part b of a launch's parts takes the b-th share of the chunks, consecutive ones, so that the record of a tensor is read once per share and
+// what follows are addresses that need no further look-up.  (A table entry per chunk, read in turn, put two dependent loads in front of
+// each chunk's own: 38 instead of 24 us for the norm of 40 M bf16 gradients.)  The first record is read ahead of pdl_wait().
+struct Share { int64_t c, end; ChunkRec chunk; TensorRec tensor; };
+__device__ __forceinline__ Share share_of(const Plan& p, int64_t from, int64_t to, int part, int parts)
+{
+    Share s;
+    s.c = from + (to - from) * part / parts;
+    s.end = from + (to - from) * (part + 1) / parts;
+    if (s.c < s.end) { s.chunk = p.chunks[s.c]; s.tensor = p.tensors[s.chunk.tensor]; }
+    return s;
+}
+// f(index of the tensor, its record, first value of the share's part of it, end of that part)
+template <typename F>
+__device__ __forceinline__ void walk(const Plan& p, Share& s, F&& f)
+{
+    while (s.c < s.end) {
+        const int64_t here = min((s.tensor.n + kChunk - 1) / kChunk - s.chunk.index, s.end - s.c);
+        f(s.chunk.tensor, s.tensor, (int64_t)s.chunk.index * kChunk, min((s.chunk.index + here) * kChunk, s.tensor.n));
+        s.c += here;
+        if (s.c < s.end) { s.chunk = p.chunks[s.c]; s.tensor = p.tensors[s.chunk.tensor]; }
     }
 }
 
 // ---- one step ----------------------------------------------------------------------------------------------
-struct StepShared { float lr1_over_lr, r2, lr, factor; int skip; };
+struct StepNow { float lr1_over_lr, r2, lr, factor, b1, b2, omb1, omb2, eps, one; };
+
+// m and sqrt(v) of a step from those before it and the gradient
+__device__ __forceinline__ void moments_8(const StepNow& k, float g, float& m, float& root)
+{
+    g = __fmul_rn(g, k.factor);
+    m = __fadd_rn(__fmul_rn(m, k.b1), __fmul_rn(g, k.omb1));
+    root = __fsqrt_rn(__fadd_rn(__fmul_rn(__fmul_rn(root, root), k.b2), __fmul_rn(__fmul_rn(g, g), k.omb2)));
+}
 
 // A warp's 256 values
 template <int BITS, bool VEC>
-__device__ __forceinline__ void step_block(const Plan& p, const TensorRec& t, const void* grad, const StepShared& k, int64_t at, int count, int lane)
+__device__ __forceinline__ void step_block(const TensorRec& t, int param_type, int grad_type, bool has_master, const void* grad, const StepNow& k, int64_t at, int count, int lane)
 {
-    const bool has_master = t.master != nullptr;
     const void* from = has_master ? (const void*)t.master : t.param;
-    const int from_type = has_master ? ST_F32 : t.param_type;
+    const int from_type = has_master ? ST_F32 : param_type;
     Raw rg, rp, rm, rv;
-    fetch<VEC>(rg, grad, t.grad_type, at, count, lane);
+    fetch<VEC>(rg, grad, grad_type, at, count, lane);
     fetch<VEC>(rp, from, from_type, at, count, lane);
     float m_scale = 0.f, v_scale = 0.f;
     const int64_t block = at / kBlockVals;
@@ -228,7 +289,7 @@ __device__ __forceinline__ void step_block(const Plan& p, const TensorRec& t, co
     }
     const float lr = k.lr * t.lr_scale, lr1 = lr * k.lr1_over_lr, decay = lr * t.wd;
     float g[kPer], x[kPer], m[kPer], root[kPer], v[kPer];
-    convert<VEC>(g, rg, t.grad_type);
+    convert<VEC>(g, rg, grad_type);
     convert<VEC>(x, rp, from_type);
     if (BITS == 32) {
         convert<VEC>(m, rm, ST_F32);
@@ -236,8 +297,8 @@ __device__ __forceinline__ void step_block(const Plan& p, const TensorRec& t, co
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const float gj = g[j] * k.factor;
-            m[j] = fmaf(p.b1, m[j], p.omb1 * gj);
-            v[j] = fmaf(p.b2, v[j], p.omb2 * gj * gj);
+            m[j] = fmaf(k.b1, m[j], k.omb1 * gj);
+            v[j] = fmaf(k.b2, v[j], k.omb2 * gj * gj);
             root[j] = __fsqrt_rn(v[j]);
         }
         put<VEC>(m, t.m, ST_F32, at, count, lane);
@@ -246,53 +307,228 @@ __device__ __forceinline__ void step_block(const Plan& p, const TensorRec& t, co
         decode<VEC>(m, root, rm, rv, m_scale, v_scale);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            const float gj = __fmul_rn(g[j], k.factor);
-            m[j] = __fadd_rn(__fmul_rn(m[j], p.b1), __fmul_rn(gj, p.omb1));
-            root[j] = __fsqrt_rn(__fadd_rn(__fmul_rn(__fmul_rn(root[j], root[j]), p.b2), __fmul_rn(__fmul_rn(gj, gj), p.omb2)));
+            moments_8(k, g[j], m[j], root[j]);
         }
-        int cm[kPer], cv[kPer];
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const float kept = fmaf(-decay, x[j], x[j]);
+        // 8 bits: the quotient to 2^-22 of itself (the arithmetic units bound that form, and its moments are 1 per cent apart)
+        const float den = fmaf(root[j], k.r2, k.eps);
+        x[j] = fmaf(-lr1, BITS == 32 ? __fdiv_rn(m[j], den) : __fdividef(m[j], den), kept);
+    }
+    put<VEC>(x, t.param, param_type, at, count, lane);
+    if (has_master) put<VEC>(x, t.master, ST_F32, at, count, lane);
+    if (BITS == 8) {
+        uint32_t cm[kPer], cv[kPer];
         encode(m, root, cm, cv, m_scale, v_scale);
         put_codes<VEC>(cm, t.m, at, count, lane);
         put_codes<VEC>(cv, t.v, at, count, lane);
         if (lane == 0) { t.m_scale[block] = m_scale; t.v_scale[block] = v_scale; }
     }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const float kept = fmaf(-decay, x[j], x[j]);
-        x[j] = fmaf(-lr1, __fdiv_rn(m[j], fmaf(root[j], k.r2, p.eps)), kept);
-    }
-    put<VEC>(x, t.param, t.param_type, at, count, lane);
-    if (has_master) put<VEC>(x, t.master, ST_F32, at, count, lane);
 }
 
-__device__ __forceinline__ bool grad_aligned(const void* grad, int type) { return ((uintptr_t)grad & (type == ST_F32 ? 15u : 7u)) == 0; }
+__device__ __forceinline__ bool grad_aligned(const void* grad, int type) { return ((uintptr_t)grad & (type == ST_F32 ? 31u : 15u)) == 0; }
 
-template <int BITS>
-__global__ void __launch_bounds__(kThreads) adamw_step_kernel(const Plan p, float grad_scale, int with_norm)
+// Two fp32 operations in one instruction, each rounded by itself
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(f32x2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+// a + b where both are products that are rounded by themselves: the assembler makes one fused operation of mul.rn.f32x2 and add.rn.f32x2, but
+// not of a product and a multiplication by a factor that it does not know (`one` is 1)
+__device__ __forceinline__ f32x2 sum2(f32x2 a, f32x2 b, f32x2 one) { return fma2(a, one, b); }
+__device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
+__device__ __forceinline__ float approximate_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float approximate_rsqrt(float x) { float y; asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// The 8-bit step of whole blocks: the same results for the moments as step_block<8>, with fewer instructions, whose issue bounds it.
+// Pairs of values go through one instruction; square roots are approximate (2^-23 of themselves: parameters need no more, and a level only
+// next to a border, where exact_codes decides).
+struct Loads8 { Raw g, p, m, v; float m_scale, v_scale; };
+template <int PARAM, int GRAD, bool MASTER>
+__device__ __forceinline__ void fetch_8(Loads8& l, const TensorRec& t, const void* grad, int64_t at, int lane)
 {
-    __shared__ StepShared k;
+    fetch<true>(l.g, grad, GRAD, at, kBlockVals, lane);
+    fetch_codes<true>(l.m, t.m, at, kBlockVals, lane);
+    fetch_codes<true>(l.v, t.v, at, kBlockVals, lane);
+    l.m_scale = t.m_scale[at / kBlockVals];
+    l.v_scale = t.v_scale[at / kBlockVals];
+    if (MASTER) fetch<true>(l.p, t.master, ST_F32, at, kBlockVals, lane);
+    else fetch<true>(l.p, t.param, PARAM, at, kBlockVals, lane);
+}
+// A lane's codes of a block, exactly, from what the block's step reads (old codes and scales, which must not have been overwritten) and the
+// reciprocals of its new scales.  Out of line: a lane in 300 comes here, and its registers are not the step's.
+template <int GRAD>
+__device__ __noinline__ uint4 exact_codes(const TensorRec* t, const void* grad, StepNow k, int64_t at, float im, float iv)
+{
+    const int lane = threadIdx.x % 32;
+    Raw rg, rm, rv;
+    float g[kPer], m[kPer], root[kPer];
+    fetch<true>(rg, grad, GRAD, at, kBlockVals, lane);
+    fetch_codes<true>(rm, t->m, at, kBlockVals, lane);
+    fetch_codes<true>(rv, t->v, at, kBlockVals, lane);
+    convert<true>(g, rg, GRAD);
+    decode<true>(m, root, rm, rv, t->m_scale[at / kBlockVals], t->v_scale[at / kBlockVals]);
+    uint32_t cm[kPer], cv[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        moments_8(k, g[j], m[j], root[j]);
+        cm[j] = __float_as_uint(copysignf(exact_level(__fmul_rn(fabsf(m[j]), im)), m[j]) + kRound);
+        cv[j] = __float_as_uint(fmaxf(exact_level(__fmul_rn(root[j], iv)), __saturatef(root[j] * FLT_MAX)) + kRound);
+    }
+    return make_uint4(low_bytes(cm), low_bytes(cm + 4), low_bytes(cv), low_bytes(cv + 4));
+}
+
+template <int PARAM, int GRAD, bool MASTER>
+__device__ __forceinline__ void step_block_8(const TensorRec* record, const TensorRec& t, const void* grad, const Loads8& l, const StepNow& k, int64_t at, int lane)
+{
+    constexpr int kPairs = kPer / 2;
+    float root[kPer], m[kPer];
+    // the largest |m| and v of the block (bits of values that are not negative are in the values' order, NaN above infinity)
+    uint32_t top = 0, top_v = 0;
+    {
+        float g[kPer];
+        convert<true>(g, l.g, GRAD);
+        const f32x2 ms = both(l.m_scale), vs = both(l.v_scale), factor = both(k.factor), b1 = both(k.b1), b2 = both(k.b2), omb1 = both(k.omb1), omb2 = both(k.omb2), one = both(k.one);
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+            const float c0 = code<true>(l.m, 2 * q, 0x80808080u, 8388608.f + 128.f), c1 = code<true>(l.m, 2 * q + 1, 0x80808080u, 8388608.f + 128.f);
+            const f32x2 d = pack2(code<true>(l.v, 2 * q, 0u, 8388608.f), code<true>(l.v, 2 * q + 1, 0u, 8388608.f));
+            const f32x2 gj = mul2(pack2(g[2 * q], g[2 * q + 1]), factor);
+            const f32x2 mj = sum2(mul2(mul2(pack2(__fmul_rn(c0, fabsf(c0)), __fmul_rn(c1, fabsf(c1))), ms), b1), mul2(gj, omb1), one);
+            const f32x2 r = mul2(mul2(d, d), vs);
+            float v0, v1;
+            unpack2(sum2(mul2(mul2(r, r), b2), mul2(mul2(gj, gj), omb2), one), v0, v1);
+            unpack2(mj, m[2 * q], m[2 * q + 1]);
+            top = max(top, max(__float_as_uint(m[2 * q]) & 0x7fffffffu, __float_as_uint(m[2 * q + 1]) & 0x7fffffffu));
+            top_v = max(top_v, max(__float_as_uint(v0), __float_as_uint(v1)));
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(root[2 * q]) : "f"(v0));
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(root[2 * q + 1]) : "f"(v1));
+        }
+    }
+    // the two scales and their reciprocals, m's in the lower lanes and v's in the upper ones: one division and one reciprocal for both
+    const float a = __uint_as_float(__reduce_max_sync(0xffffffffu, top)), b = __fsqrt_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, top_v)));
+    const bool low = lane < 16;
+    const float scale = low && a < 0x1p-100f ? 0.f : __fdiv_rn(low ? a : b, low ? 127.f * 127.f : 255.f * 255.f);    // roots are rounded in the values' order: b is the largest root
+    const float inverse = scale > 0.f ? __frcp_rn(scale) : 0.f, im = __shfl_sync(0xffffffffu, inverse, 0), iv = __shfl_sync(0xffffffffu, inverse, 16);
+    {
+        float x[kPer];
+        convert<true>(x, l.p, MASTER ? ST_F32 : PARAM);
+        const float lr = k.lr * t.lr_scale;
+        const f32x2 lr1 = both(-lr * k.lr1_over_lr), decay = both(-lr * t.wd), r2 = both(k.r2), eps = both(k.eps);
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+            const f32x2 xj = pack2(x[2 * q], x[2 * q + 1]);
+            const f32x2 kept = fma2(decay, xj, xj);
+            float d0, d1;
+            unpack2(fma2(pack2(root[2 * q], root[2 * q + 1]), r2, eps), d0, d1);
+            // the quotient to 2^-22 of itself: the moments are 1 per cent apart
+            const f32x2 u = mul2(pack2(m[2 * q], m[2 * q + 1]), pack2(approximate_reciprocal(d0), approximate_reciprocal(d1)));
+            unpack2(fma2(lr1, u, kept), x[2 * q], x[2 * q + 1]);
+        }
+        put<true>(x, t.param, PARAM, at, kBlockVals, lane);
+        if (MASTER) put<true>(x, t.master, ST_F32, at, kBlockVals, lane);
+    }
+    uint32_t cm[kPer], cv[kPer];
+    float far = 0.f;
+    const f32x2 im2 = both(im), iv2 = both(iv), up = both(kRound), down = both(-kRound), minus = both(-1.f);
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) {
+        float t0, t1, r0, r1, e0, e1;
+        unpack2(mul2(pack2(m[2 * q], m[2 * q + 1]), im2), t0, t1);
+        unpack2(mul2(pack2(root[2 * q], root[2 * q + 1]), iv2), r0, r1);
+        const f32x2 s = pack2(copysignf(approximate_root(fabsf(t0)), t0), copysignf(approximate_root(fabsf(t1)), t1));
+        const f32x2 r = pack2(fmaxf(approximate_root(r0), __saturatef(root[2 * q] * FLT_MAX)), fmaxf(approximate_root(r1), __saturatef(root[2 * q + 1] * FLT_MAX)));
+        const f32x2 y = add2(s, up), z = add2(r, up);
+        unpack2(fma2(add2(y, down), minus, s), e0, e1);
+        far = fmaxf(far, fmaxf(fabsf(e0), fabsf(e1)));
+        unpack2(fma2(add2(z, down), minus, r), e0, e1);
+        far = fmaxf(far, fmaxf(fabsf(e0), fabsf(e1)));
+        cm[2 * q] = (uint32_t)y; cm[2 * q + 1] = (uint32_t)(y >> 32);
+        cv[2 * q] = (uint32_t)z; cv[2 * q + 1] = (uint32_t)(z >> 32);
+    }
+    uint4 codes = make_uint4(low_bytes(cm), low_bytes(cm + 4), low_bytes(cv), low_bytes(cv + 4));
+    if (far > 0.5f - kNear) codes = exact_codes<GRAD>(record, grad, k, at, im, iv);
+    __syncwarp();                                               // nobody reads the old scales any more
+    *(uint2*)((uint8_t*)t.m + at + kPer * lane) = make_uint2(codes.x, codes.y);
+    *(uint2*)((uint8_t*)t.v + at + kPer * lane) = make_uint2(codes.z, codes.w);
+    if ((lane & 15) == 0) (low ? t.m_scale : t.v_scale)[at / kBlockVals] = scale;
+}
+
+// All whole blocks of a tensor's part; returns where it stopped.  A function of its own for each combination of types: the conversions
+// are decided outside the loop, and the registers are this loop's alone (inlined into the walk, with all combinations side by
+// side, the 8-bit step of 200 M bf16 values took 738 us instead of 545).  With 8-bit moments, where a warp has much to work out, the next
+// block's loads are on their way meanwhile.
+template <int BITS, int PARAM, int GRAD, bool MASTER>
+__device__ __noinline__ int64_t step_blocks(const TensorRec* record, const void* grad, StepNow k, int64_t at, int64_t end)
+{
+    const int lane = threadIdx.x % 32;
+    const TensorRec t = *record;
+    if (BITS == 8) {
+        Loads8 now;
+        for (; at + kBlockVals <= end; at += kChunk) {
+            fetch_8<PARAM, GRAD, MASTER>(now, t, grad, at, lane);
+            step_block_8<PARAM, GRAD, MASTER>(record, t, grad, now, k, at, lane);
+        }
+    } else {
+        for (; at + kBlockVals <= end; at += kChunk) step_block<32, true>(t, PARAM, GRAD, MASTER, grad, k, at, kBlockVals, lane);
+    }
+    return at;
+}
+template <int BITS, int PARAM, bool MASTER, typename... A>
+__device__ __forceinline__ int64_t step_blocks_of(int grad_type, const A&... a)
+{
+    return grad_type == ST_F32 ? step_blocks<BITS, PARAM, ST_F32, MASTER>(a...) : grad_type == ST_BF16 ? step_blocks<BITS, PARAM, ST_BF16, MASTER>(a...)
+                                                                                                      : step_blocks<BITS, PARAM, ST_F16, MASTER>(a...);
+}
+template <int BITS, bool MASTER, typename... A>
+__device__ __forceinline__ int64_t step_blocks_of(int param_type, int grad_type, const A&... a)
+{
+    return param_type == ST_F32 ? step_blocks_of<BITS, ST_F32, MASTER>(grad_type, a...) : param_type == ST_BF16 ? step_blocks_of<BITS, ST_BF16, MASTER>(grad_type, a...)
+                                                                                                             : step_blocks_of<BITS, ST_F16, MASTER>(grad_type, a...);
+}
+
+// The path of single values, out of line: its registers are not the vector path's
+template <int BITS>
+__device__ __noinline__ void step_block_slow(const TensorRec* t, const void* grad, StepNow k, int64_t at, int lane)
+{
+    step_block<BITS, false>(*t, t->param_type, t->grad_type, t->master != nullptr, grad, k, at, (int)min(t->n - at, (int64_t)kBlockVals), lane);
+}
+
+__device__ __forceinline__ void bias_corrections(const Plan& p, long long t, float (&out)[2])
+{
+    out[0] = (float)(-1.0 / expm1((double)t * p.ln_b1));
+    out[1] = (float)(1.0 / sqrt(-expm1((double)t * p.ln_b2)));
+}
+
+// Block 0 works the next step's bias corrections out (two exponentials in double, over a microsecond); the others step the tensors.
+template <int BITS>
+__global__ void __launch_bounds__(kThreads, BITS == 32 ? 4 : 5) adamw_step_kernel(const __grid_constant__ Plan p, float grad_scale, int with_norm)
+{
+    Share share;
+    if (blockIdx.x) share = share_of(p, 0, p.n_chunks, blockIdx.x - 1, gridDim.x - 1);
     pdl_wait();
     pdl_launch_dependents();
-    if (threadIdx.x == 0) {
-        const double t = (double)(p.sc->t + 1), lr = p.sc->lr;
-        k.lr = (float)lr;
-        k.lr1_over_lr = (float)(-1.0 / expm1(t * p.ln_b1));
-        k.r2 = (float)(1.0 / sqrt(-expm1(t * p.ln_b2)));
-        k.factor = with_norm ? p.sc->factor : grad_scale;
-        k.skip = with_norm && p.sc->skip;
-    }
-    __syncthreads();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (!k.skip) {
-        for (int64_t c = blockIdx.x; c < p.n_chunks; c += gridDim.x) {
-            const ChunkRec ck = p.chunks[p.n_chunks - 1 - c];
-            const TensorRec& t = p.tensors[ck.tensor];
-            const void* grad = t.grad;
-            const int64_t at = (int64_t)ck.index * kChunk + warp * kBlockVals, left = t.n - at;
-            if (!grad || left <= 0) continue;
-            if (left >= kBlockVals && t.vec && grad_aligned(grad, t.grad_type)) step_block<BITS, true>(p, t, grad, k, at, kBlockVals, lane);
-            else step_block<BITS, false>(p, t, grad, k, at, (int)min(left, (int64_t)kBlockVals), lane);
-        }
+    const long long t = p.sc->t + 1;                    // every thread reads it: the step that is taken
+    const bool skip = with_norm && p.sc->skip;
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0 && !skip) bias_corrections(p, t + 1, p.sc->bias[(t + 1) & 1]);
+    } else if (!skip) {
+        const StepNow k = {p.sc->bias[t & 1][0], p.sc->bias[t & 1][1], (float)p.sc->lr, with_norm ? p.sc->factor : grad_scale,
+                           p.b1, p.b2, p.omb1, p.omb2, p.eps, p.one};
+        const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+        walk(p, share, [&](int i, const TensorRec& t, int64_t begin, int64_t end) {
+            const void* grad = p.grads[i];
+            if (!grad) return;
+            int64_t at = begin + warp * kBlockVals;
+            if (t.vec && grad_aligned(grad, t.grad_type))
+                at = t.master ? step_blocks_of<BITS, true>(t.param_type, t.grad_type, p.tensors + i, grad, k, at, end)
+                              : step_blocks_of<BITS, false>(t.param_type, t.grad_type, p.tensors + i, grad, k, at, end);
+            for (; at < end; at += kChunk) step_block_slow<BITS>(p.tensors + i, grad, k, at, lane);
+        });
     }
     // the block that finishes last counts the step: every block has read the count by then
     __syncthreads();
@@ -300,7 +536,7 @@ __global__ void __launch_bounds__(kThreads) adamw_step_kernel(const Plan p, floa
         __threadfence();
         if (atomicAdd(&p.sc->step_ticket, 1u) == gridDim.x - 1) {
             p.sc->step_ticket = 0;
-            if (!k.skip) p.sc->t += 1;
+            if (!skip) p.sc->t = t;
         }
     }
 }
@@ -318,27 +554,39 @@ __device__ __forceinline__ double block_sum(double x, double (&shared)[kWarps])
     return x;
 }
 
-__global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const Plan p, float grad_scale, float* norm_out)
+__global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_constant__ Plan p, float grad_scale, float* norm_out)
 {
     __shared__ double shared[kWarps];
     __shared__ bool last;
+    Share share = share_of(p, 0, p.n_chunks, blockIdx.x, gridDim.x);
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     double sum = 0;
-    for (int64_t c = blockIdx.x; c < p.n_chunks; c += gridDim.x) {
-        const ChunkRec ck = p.chunks[c];
-        const TensorRec& t = p.tensors[ck.tensor];
-        const void* grad = t.grad;
-        const int64_t at = (int64_t)ck.index * kChunk + warp * kBlockVals, left = t.n - at;
-        if (!grad || left <= 0) continue;
-        Raw r;
+    const auto add = [&](const Raw& r, int type, auto vec) {
         float g[kPer];
-        if (left >= kBlockVals && grad_aligned(grad, t.grad_type)) { fetch<true>(r, grad, t.grad_type, at, kBlockVals, lane); convert<true>(g, r, t.grad_type); }
-        else { fetch<false>(r, grad, t.grad_type, at, (int)min(left, (int64_t)kBlockVals), lane); convert<false>(g, r, t.grad_type); }
+        convert<decltype(vec)::value>(g, r, type);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) { const double d = g[j]; sum = fma(d, d, sum); }
-    }
+    };
+    walk(p, share, [&](int i, const TensorRec& t, int64_t begin, int64_t end) {
+        const void* grad = p.grads[i];
+        if (!grad) return;
+        const int type = t.grad_type;
+        int64_t at = begin + warp * kBlockVals;
+        if (grad_aligned(grad, type)) {
+            constexpr int kFlight = 4;          // a warp's blocks whose loads are on their way together
+            for (; at + (kFlight - 1) * kChunk + kBlockVals <= end; at += kFlight * kChunk) {
+                Raw r[kFlight];
+#pragma unroll
+                for (int u = 0; u < kFlight; ++u) fetch<true>(r[u], grad, type, at + u * kChunk, kBlockVals, lane);
+#pragma unroll
+                for (int u = 0; u < kFlight; ++u) add(r[u], type, std::true_type{});
+            }
+            for (; at + kBlockVals <= end; at += kChunk) { Raw r; fetch<true>(r, grad, type, at, kBlockVals, lane); add(r, type, std::true_type{}); }
+        }
+        for (; at < end; at += kChunk) { Raw r; fetch<false>(r, grad, type, at, (int)min(end - at, (int64_t)kBlockVals), lane); add(r, type, std::false_type{}); }
+    });
     sum = block_sum(sum, shared);
     if (threadIdx.x == 0) {
         p.partials[blockIdx.x] = sum;
@@ -365,88 +613,105 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const Plan p, floa
 constexpr int kPointers = 448;      // of one launch: with the rest of the arguments inside the 4 KB that any launch may carry
 struct PointerArgs { const void* q[kPointers]; };
 
-__global__ void adamw_set_grads_kernel(TensorRec* tensors, int first, int count, const PointerArgs a)
+__global__ void adamw_set_grads_kernel(const void** grads, int first, int count, const PointerArgs a)
 {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < count) tensors[first + i].grad = a.q[i];
+    if (i < count) grads[first + i] = a.q[i];
 }
 __global__ void adamw_set_lr_kernel(Scalars* sc, double lr) { sc->lr = lr; }
 
 // ---- moments as fp32 values and back -----------------------------------------------------------------------
-// Tensors [first, first + count) with their pointers in the arguments: m's at 2 i, v's at 2 i + 1
-__device__ __forceinline__ bool moment_block(const Plan& p, int64_t c, int first, int warp, TensorRec& t, int& i, int64_t& at, int& count)
+// Tensors [first, ...) of chunks [chunk_begin, chunk_end) with their pointers in the arguments: m's at 2 i, v's at 2 i + 1
+struct Moments { Raw m, v; float m_scale, v_scale; };
+template <int BITS, bool VEC>
+__device__ __forceinline__ void fetch_moments(Moments& l, const TensorRec& t, int64_t at, int count, int lane)
 {
-    const ChunkRec ck = p.chunks[c];
-    t = p.tensors[ck.tensor];
-    i = ck.tensor - first;
-    at = (int64_t)ck.index * kChunk + warp * kBlockVals;
-    const int64_t left = t.n - at;
-    count = (int)min(left, (int64_t)kBlockVals);
-    return left > 0;
+    if (BITS == 32) {
+        fetch<VEC>(l.m, t.m, ST_F32, at, count, lane);
+        fetch<VEC>(l.v, t.v, ST_F32, at, count, lane);
+    } else {
+        fetch_codes<VEC>(l.m, t.m, at, count, lane);
+        fetch_codes<VEC>(l.v, t.v, at, count, lane);
+        l.m_scale = t.m_scale[at / kBlockVals];
+        l.v_scale = t.v_scale[at / kBlockVals];
+    }
 }
-
-template <int BITS>
-__global__ void __launch_bounds__(kThreads) adamw_read_kernel(const Plan p, int first, int64_t chunk_begin, int64_t chunk_end, const PointerArgs a)
+template <int BITS, bool VEC>
+__device__ __forceinline__ void put_moments(const Moments& l, float* m_out, float* v_out, int64_t at, int count, int lane)
 {
+    float m[kPer], v[kPer];
+    if (BITS == 32) {
+        convert<VEC>(m, l.m, ST_F32);
+        convert<VEC>(v, l.v, ST_F32);
+    } else {
+        decode<VEC>(m, v, l.m, l.v, l.m_scale, l.v_scale);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v[j] = __fmul_rn(v[j], v[j]);
+    }
+    if (m_out) put<VEC>(m, m_out, ST_F32, at, count, lane);
+    if (v_out) put<VEC>(v, v_out, ST_F32, at, count, lane);
+}
+template <int BITS>
+__global__ void __launch_bounds__(kThreads) adamw_read_kernel(const __grid_constant__ Plan p, int first, int64_t chunk_begin, int64_t chunk_end, const __grid_constant__ PointerArgs a)
+{
+    Share share = share_of(p, chunk_begin, chunk_end, blockIdx.x, gridDim.x);
     pdl_wait();
     pdl_launch_dependents();
+    constexpr int kFlight = BITS == 8 ? 2 : 1;          // a warp's blocks whose loads are on their way together
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    for (int64_t c = chunk_begin + blockIdx.x; c < chunk_end; c += gridDim.x) {
-        TensorRec t; int i, count; int64_t at;
-        if (!moment_block(p, c, first, warp, t, i, at, count)) continue;
-        float* out[2] = {(float*)a.q[2 * i], (float*)a.q[2 * i + 1]};
-        float m[kPer], v[kPer];
-        Raw rm, rv;
-        const bool vec = count == kBlockVals && t.vec && (((uintptr_t)out[0] | (uintptr_t)out[1]) & 15) == 0;
-        if (BITS == 32) {
-            if (vec) { fetch<true>(rm, t.m, ST_F32, at, count, lane); fetch<true>(rv, t.v, ST_F32, at, count, lane); convert<true>(m, rm, ST_F32); convert<true>(v, rv, ST_F32); }
-            else { fetch<false>(rm, t.m, ST_F32, at, count, lane); fetch<false>(rv, t.v, ST_F32, at, count, lane); convert<false>(m, rm, ST_F32); convert<false>(v, rv, ST_F32); }
-        } else {
-            const float ms = t.m_scale[at / kBlockVals], vs = t.v_scale[at / kBlockVals];
-            if (vec) { fetch_codes<true>(rm, t.m, at, count, lane); fetch_codes<true>(rv, t.v, at, count, lane); decode<true>(m, v, rm, rv, ms, vs); }
-            else { fetch_codes<false>(rm, t.m, at, count, lane); fetch_codes<false>(rv, t.v, at, count, lane); decode<false>(m, v, rm, rv, ms, vs); }
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) v[j] = __fmul_rn(v[j], v[j]);
-        }
+    walk(p, share, [&](int i, const TensorRec& t, int64_t begin, int64_t end) {
+        float *m_out = (float*)a.q[2 * (i - first)], *v_out = (float*)a.q[2 * (i - first) + 1];
+        const bool vec = t.vec && (((uintptr_t)m_out | (uintptr_t)v_out) & 31) == 0;
+        int64_t at = begin + warp * kBlockVals;
+        Moments l[kFlight];
         if (vec) {
-            if (out[0]) put<true>(m, out[0], ST_F32, at, count, lane);
-            if (out[1]) put<true>(v, out[1], ST_F32, at, count, lane);
-        } else {
-            if (out[0]) put<false>(m, out[0], ST_F32, at, count, lane);
-            if (out[1]) put<false>(v, out[1], ST_F32, at, count, lane);
+            for (; at + (kFlight - 1) * kChunk + kBlockVals <= end; at += kFlight * kChunk) {
+#pragma unroll
+                for (int u = 0; u < kFlight; ++u) fetch_moments<BITS, true>(l[u], t, at + u * kChunk, kBlockVals, lane);
+#pragma unroll
+                for (int u = 0; u < kFlight; ++u) put_moments<BITS, true>(l[u], m_out, v_out, at + u * kChunk, kBlockVals, lane);
+            }
+            for (; at + kBlockVals <= end; at += kChunk) { fetch_moments<BITS, true>(l[0], t, at, kBlockVals, lane); put_moments<BITS, true>(l[0], m_out, v_out, at, kBlockVals, lane); }
         }
-    }
+        for (; at < end; at += kChunk) {
+            const int count = (int)min(end - at, (int64_t)kBlockVals);
+            fetch_moments<BITS, false>(l[0], t, at, count, lane);
+            put_moments<BITS, false>(l[0], m_out, v_out, at, count, lane);
+        }
+    });
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(kThreads) adamw_write_kernel(const Plan p, int first, int64_t chunk_begin, int64_t chunk_end, const PointerArgs a)
+__global__ void __launch_bounds__(kThreads) adamw_write_kernel(const __grid_constant__ Plan p, int first, int64_t chunk_begin, int64_t chunk_end, const __grid_constant__ PointerArgs a)
 {
+    Share share = share_of(p, chunk_begin, chunk_end, blockIdx.x, gridDim.x);
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    for (int64_t c = chunk_begin + blockIdx.x; c < chunk_end; c += gridDim.x) {
-        TensorRec t; int i, count; int64_t at;
-        if (!moment_block(p, c, first, warp, t, i, at, count)) continue;
-        const float* in[2] = {(const float*)a.q[2 * i], (const float*)a.q[2 * i + 1]};
-        float m[kPer] = {}, v[kPer] = {};
-        Raw r;
-        if (in[0]) { fetch<false>(r, in[0], ST_F32, at, count, lane); convert<false>(m, r, ST_F32); }
-        if (in[1]) { fetch<false>(r, in[1], ST_F32, at, count, lane); convert<false>(v, r, ST_F32); }
+    walk(p, share, [&](int i, const TensorRec& t, int64_t begin, int64_t end) {
+        const float *m_in = (const float*)a.q[2 * (i - first)], *v_in = (const float*)a.q[2 * (i - first) + 1];
+        for (int64_t at = begin + warp * kBlockVals; at < end; at += kChunk) {
+            const int count = (int)min(t.n - at, (int64_t)kBlockVals);
+            float m[kPer] = {}, v[kPer] = {};
+            Raw r;
+            if (m_in) { fetch<false>(r, m_in, ST_F32, at, count, lane); convert<false>(m, r, ST_F32); }
+            if (v_in) { fetch<false>(r, v_in, ST_F32, at, count, lane); convert<false>(v, r, ST_F32); }
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];
-        if (BITS == 32) {
-            if (in[0]) put<false>(m, t.m, ST_F32, at, count, lane);
-            if (in[1]) put<false>(v, t.v, ST_F32, at, count, lane);
-        } else {
+            for (int j = 0; j < kPer; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];
+            if (BITS == 32) {
+                if (m_in) put<false>(m, t.m, ST_F32, at, count, lane);
+                if (v_in) put<false>(v, t.v, ST_F32, at, count, lane);
+            } else {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) v[j] = __fsqrt_rn(v[j]);
-            int cm[kPer], cv[kPer];
-            float ms, vs;
-            encode(m, v, cm, cv, ms, vs);
-            if (in[0]) { put_codes<false>(cm, t.m, at, count, lane); if (lane == 0) t.m_scale[at / kBlockVals] = ms; }
-            if (in[1]) { put_codes<false>(cv, t.v, at, count, lane); if (lane == 0) t.v_scale[at / kBlockVals] = vs; }
+                for (int j = 0; j < kPer; ++j) v[j] = __fsqrt_rn(v[j]);
+                uint32_t cm[kPer], cv[kPer];
+                float ms, vs;
+                encode(m, v, cm, cv, ms, vs);
+                if (m_in) { put_codes<false>(cm, t.m, at, count, lane); if (lane == 0) t.m_scale[at / kBlockVals] = ms; }
+                if (v_in) { put_codes<false>(cv, t.v, at, count, lane); if (lane == 0) t.v_scale[at / kBlockVals] = vs; }
+            }
         }
-    }
+    });
 }
 
 }  // namespace
@@ -459,7 +724,7 @@ struct st_adamw {
     Plan plan = {};
     int device = 0, n = 0, bits = 32;
     cudaStream_t stream = nullptr;
-    int step_grid = 0, norm_grid = 0, any_grid = 0;
+    int step_grid = 0, norm_grid = 0, moments_span = 0, moments_resident = 0;
     bool always_norm = false;
     void* block = nullptr;                  // the one allocation: scalars, partial sums, tables
     std::vector<int64_t> first_chunk;       // [n + 1]
@@ -553,7 +818,7 @@ st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adam
         total += t.n;
         o->values[i] = t.n; o->grad_type[i] = (uint8_t)t.grad_type;
         o->first_chunk[i + 1] = o->first_chunk[i] + (t.n + kChunk - 1) / kChunk;
-        r = TensorRec{t.param, t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.n, t.weight_decay, t.lr_scale,
+        r = TensorRec{t.param, t.master, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.n, t.weight_decay, t.lr_scale,
                       (uint8_t)t.param_type, (uint8_t)t.grad_type, 0, 0};
         if (t.n == 0) continue;
         const size_t moment = d.state_bits == 32 ? 4 : 1, scales = 4 * (size_t)((t.n + kBlockVals - 1) / kBlockVals);
@@ -569,8 +834,7 @@ st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adam
             if (const char* f = buffer_fault(b.q, b.element, o->device)) return fail(nullptr, ST_ERR_INVALID_ARG, "st_adamw_create: tensor %d: %s %s", i, b.name, f);
             o->written.push_back({(uintptr_t)b.q, (uintptr_t)b.q + b.bytes});
         }
-        const size_t four = d.state_bits == 32 ? 16 : 4;
-        r.vec = aligned(t.param, 4 * type_size(t.param_type)) && aligned(t.master, 16) && aligned(t.exp_avg, four) && aligned(t.exp_avg_sq, four);
+        r.vec = aligned(t.param, kPer * type_size(t.param_type)) && aligned(t.master, kPer * 4) && aligned(t.exp_avg, kPer * moment) && aligned(t.exp_avg_sq, kPer * moment);
     }
     std::sort(o->written.begin(), o->written.end(), [](const st_adamw::Range& a, const st_adamw::Range& b) { return a.begin < b.begin; });
     for (size_t i = 1; i < o->written.size(); ++i)
@@ -584,29 +848,47 @@ st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adam
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&step, d.state_bits == 32 ? adamw_step_kernel<32> : adamw_step_kernel<8>, kThreads, 0);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&norm, adamw_norm_kernel, kThreads, 0);
     if (e != cudaSuccess) { cudaGetLastError(); return fail(nullptr, ST_ERR_CUDA, "st_adamw_create: %s", cudaGetErrorString(e)); }
-    const auto grid = [&](int per_sm) { return (int)std::max<int64_t>(1, std::min<int64_t>(n_chunks, (int64_t)sms * std::max(per_sm, 1))); };
-    o->step_grid = grid(step); o->norm_grid = grid(norm); o->any_grid = grid(8);
+    // Blocks of a launch: as many as the GPU holds at once, or one per `span` chunks where that is more.  A step with fp32 moments and the reading
+    // of moments wait for memory, and short shares that the GPU hands out as blocks end keep all of it busy (150 M fp32 values with
+    // spans of 4 / 8 chunks / one share per resident block: 633 / 648 / 690 us; reading 200 M values: 327 with 8, 353).  A step with 8-bit
+    // moments and the norm wait for instructions, and a block's beginning and end cost more than an uneven end (200 M: 744 us with
+    // spans of 8, 520 with one share each; norm 77 and 63).
+    const auto blocks = [&](int per_sm, int span) {
+        const int64_t resident = (int64_t)sms * std::max(per_sm, 1), most = span ? std::max(resident, n_chunks / span) : resident;
+        return (int)std::max<int64_t>(1, std::min(n_chunks, most));
+    };
+    o->step_grid = 1 + blocks(step, d.state_bits == 32 ? 4 : 0);
+    o->norm_grid = blocks(norm, 0);
+    o->moments_span = 8; o->moments_resident = sms * 8;
 
     std::vector<ChunkRec> chunks((size_t)n_chunks);
     for (int i = 0; i < d.n_tensors; ++i)
         for (int64_t c = o->first_chunk[i]; c < o->first_chunk[i + 1]; ++c) chunks[c] = {i, (int32_t)(c - o->first_chunk[i])};
     const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     const size_t at_partials = up(sizeof(Scalars)), at_tensors = at_partials + up(sizeof(double) * o->norm_grid),
-                 at_chunks = at_tensors + up(sizeof(TensorRec) * recs.size()), bytes = at_chunks + up(sizeof(ChunkRec) * chunks.size());
+                 at_grads = at_tensors + up(sizeof(TensorRec) * recs.size()),
+                 at_chunks = at_grads + up(sizeof(void*) * recs.size()), bytes = at_chunks + up(sizeof(ChunkRec) * chunks.size());
     e = cudaMalloc(&o->block, bytes);
     if (e != cudaSuccess) { cudaGetLastError(); return fail(nullptr, e == cudaErrorMemoryAllocation ? ST_ERR_OOM : ST_ERR_CUDA, "st_adamw_create: %s", cudaGetErrorString(e)); }
     char* b = (char*)o->block;
     Plan& p = o->plan;
-    p.sc = (Scalars*)b; p.partials = (double*)(b + at_partials); p.tensors = (TensorRec*)(b + at_tensors); p.chunks = (const ChunkRec*)(b + at_chunks);
+    p.sc = (Scalars*)b; p.partials = (double*)(b + at_partials); p.tensors = (const TensorRec*)(b + at_tensors); p.grads = (const void**)(b + at_grads);
+    p.chunks = (const ChunkRec*)(b + at_chunks);
     p.n_chunks = n_chunks;
     p.ln_b1 = log(d.beta1); p.ln_b2 = log(d.beta2); p.max_norm = d.max_norm;
-    p.b1 = (float)d.beta1; p.b2 = (float)d.beta2; p.omb1 = (float)(1.0 - d.beta1); p.omb2 = (float)(1.0 - d.beta2); p.eps = (float)d.eps;
+    p.b1 = (float)d.beta1; p.b2 = (float)d.beta2; p.omb1 = (float)(1.0 - d.beta1); p.omb2 = (float)(1.0 - d.beta2); p.eps = (float)d.eps; p.one = 1.f;
     p.skip_nonfinite = d.skip_nonfinite;
     o->always_norm = d.max_norm > 0 || d.skip_nonfinite;
     Scalars sc = {};
     sc.t = d.first_step; sc.lr = d.lr; sc.factor = 1.f;
+    const double next = (double)d.first_step + 1;
+    sc.bias[(d.first_step + 1) & 1][0] = (float)(-1.0 / expm1(next * p.ln_b1));
+    sc.bias[(d.first_step + 1) & 1][1] = (float)(1.0 / sqrt(-expm1(next * p.ln_b2)));
+    std::vector<const void*> grads(d.n_tensors);
+    for (int i = 0; i < d.n_tensors; ++i) grads[i] = tensors[i].n ? tensors[i].grad : nullptr;
     const struct { void* to; const void* from; size_t bytes; } copies[] = {
-        {p.sc, &sc, sizeof sc}, {p.tensors, recs.data(), sizeof(TensorRec) * recs.size()}, {(void*)p.chunks, chunks.data(), sizeof(ChunkRec) * chunks.size()}};
+        {p.sc, &sc, sizeof sc}, {(void*)p.tensors, recs.data(), sizeof(TensorRec) * recs.size()}, {p.grads, grads.data(), sizeof(void*) * grads.size()},
+         {(void*)p.chunks, chunks.data(), sizeof(ChunkRec) * chunks.size()}};
     for (const auto& c : copies)
         if (e == cudaSuccess && c.bytes) e = cudaMemcpyAsync(c.to, c.from, c.bytes, cudaMemcpyHostToDevice, o->stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(o->stream);
@@ -633,7 +915,7 @@ st_status move_moments(st_adamw* o, const void* const* m, const void* const* v, 
         for (int i = first; i < last; ++i) { a.q[2 * (i - first)] = m ? m[i] : nullptr; a.q[2 * (i - first) + 1] = v ? v[i] : nullptr; }
         const int64_t begin = o->first_chunk[first], end = o->first_chunk[last];
         if (begin == end) continue;
-        const int grid = (int)std::min<int64_t>(end - begin, o->any_grid);
+        const int grid = (int)std::min<int64_t>(end - begin, std::max<int64_t>(o->moments_resident, (end - begin) / o->moments_span));
         auto kernel = write ? (o->bits == 32 ? adamw_write_kernel<32> : adamw_write_kernel<8>) : (o->bits == 32 ? adamw_read_kernel<32> : adamw_read_kernel<8>);
         launch_early(pdl_enabled(), kernel, dim3(grid), dim3(kThreads), 0, o->stream, o->plan, first, begin, end, a);
     }
@@ -676,7 +958,7 @@ st_status st_adamw_set_grads(st_adamw* o, const void* const* grads)
         const int count = std::min(kPointers, o->n - first);
         PointerArgs a;
         std::copy(grads + first, grads + first + count, a.q);
-        adamw_set_grads_kernel<<<(count + 127) / 128, 128, 0, o->stream>>>(o->plan.tensors, first, count, a);
+        adamw_set_grads_kernel<<<(count + 127) / 128, 128, 0, o->stream>>>(o->plan.grads, first, count, a);
     }
     return check_launch(o, "st_adamw_set_grads");
 }
