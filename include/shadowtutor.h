@@ -451,6 +451,59 @@ ST_API st_status st_adamw_step_count(st_adamw *opt, int64_t *steps);
 ST_API void st_adamw_destroy(st_adamw *opt);
 ST_API const char *st_adamw_last_error(const st_adamw *opt);
 
+/* ---- operators around the step: 8-bit integer layers of the part that is never trained -------------------- */
+
+/*
+ * st_quantize_rows — rows to 8-bit integers with one scale each: tokens or pixels of activations, output channels of weights.
+ * The frozen front part's weights do not change (Section 4.2), so they are quantised once; its activations are quantised on the way.
+ *     scale[r] = max_c |x[r][c]| / 127;   q[r][c] = x[r][c] / scale[r], rounded to the nearest whole number, halves to the even one
+ * The quotient's rounding is that of the exact quotient of the two fp32 numbers.  A row of zeros, or one whose scale is below fp32's
+ * range, has scale 0 and integers 0.  A row with a value that is not finite has scale NaN and integers 0: what is multiplied with it is NaN.
+ *   x           device; x_type (st_dtype), element (r, c) at x[r * row_stride + c * col_stride], strides >= 0.  Tokens and weights have
+ *               col_stride 1; a planar feature map [channels][h][w] has row_stride 1 and col_stride h * w: its rows are pixels.
+ *   q           device; int8 [rows][ldq], ldq >= cols; what lies between cols and ldq is left as it is.  With ldq a multiple of 16 and q
+ *               on a multiple of 16 bytes, st_int8_matmul takes its fast path.
+ *   scale       device; fp32 [rows].
+ *   rows, cols  rows >= 0, cols >= 1.
+ * Returns after enqueueing on cuda_stream (NULL = default stream), allocates nothing, and may be captured into a graph.
+ * ST_ERR_INVALID_ARG: a pointer that is not memory of the current device, unaligned to its element or overlapping q or scale; bad extents.
+ */
+ST_API st_status st_quantize_rows(const void *x, int32_t x_type, int64_t rows, int64_t cols, int64_t row_stride,
+                                  int64_t col_stride, int8_t *q, int64_t ldq, float *scale, void *cuda_stream);
+
+/*
+ * st_int8_matmul — product of 8-bit integers with a scale per token and one per output channel: a linear layer, or a 1x1 convolution
+ * over pixel-major features,
+ *     y[m][n] = act((sum_k x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n])
+ * with the sum exact in 32-bit integers, the operations behind it in fp32 in this order, and one rounding to y's type.
+ *   x, ldx      device; int8 [M][ldx], the tokens.      x_scale  device; fp32 [M].
+ *   w, ldw      device; int8 [N][ldw], the weights.     w_scale  device; fp32 [N].
+ *   bias        device; fp32 [N], or NULL.              relu     0: act is the identity; 1: max(., 0), NaN stays NaN.
+ *   y, ldy      device; [M][ldy] of y_type; what lies between N and ldy is left as it is.
+ *   M, N, K     M, N >= 0, 1 <= K <= 131071 (sums of products of -128 .. 127 stay in 32 bits).
+ * x and w may start anywhere and have any pitch; where both start at multiples of 16 bytes and have pitches that are such multiples
+ * the tensor cores do the work, otherwise a slower kernel does.  y in 16-byte steps takes the fastest stores.
+ * Results depend on the arguments alone, bit for bit.  Returns after enqueueing on cuda_stream (NULL = default stream) and may be
+ * captured into a graph; the first call on a device prepares the kernels there and must not be captured.
+ * There is no backward: gradients stop at the freeze boundary (Section 4.2), and quantised layers lie in front of it.
+ * ST_ERR_INVALID_ARG as for st_quantize_rows; ST_ERR_UNSUPPORTED: K above 131071, more than 2^31 tiles; ST_ERR_CUDA: also where an
+ * earlier product on this device gave up on a wait and left its result incomplete.
+ */
+ST_API st_status st_int8_matmul(const int8_t *x, int64_t ldx, const float *x_scale, const int8_t *w, int64_t ldw,
+                                const float *w_scale, const float *bias, int32_t relu, int64_t M, int64_t N, int64_t K,
+                                void *y, int32_t y_type, int64_t ldy, void *cuda_stream);
+
+/*
+ * st_set_frozen_features_int8 — the frozen front part's last pointwise layer in 8 bits, straight into the feature cache of a stream: what
+ * st_set_frozen_features stores, computed by st_int8_matmul from the layer's quantised input, without a feature map in between.
+ *   x, ldx, x_scale   the layer's input, a pixel per row (feat_h * feat_w rows, row-major over the map), K channels.
+ *   w, ldw, w_scale   the layer's weights, c_in rows.   bias, relu as in st_int8_matmul.
+ * Works on the context's stream.  ST_ERR_UNSUPPORTED with gemm_precision 0 (the cache is then fp32 planes).
+ */
+ST_API st_status st_set_frozen_features_int8(st_ctx *ctx, int32_t stream, const int8_t *x, int64_t ldx, const float *x_scale,
+                                             const int8_t *w, int64_t ldw, const float *w_scale, const float *bias,
+                                             int32_t relu, int64_t K);
+
 /* ---- host-side pieces around the step: no device work, callable without a GPU ------------------------ */
 
 /*

@@ -44,6 +44,7 @@ EXPORTED = [
     "st_traffic_bounds", "st_choose_max_updates", "st_apply_update", "st_measure_arithmetic_peaks",
     "st_prefetch_key_frame", "st_use_prefetched_key_frame", "st_head_param_counts", "st_set_skip_features",
     "st_adamw_create", "st_adamw_set_grads", "st_adamw_set_lr", "st_adamw_step", "st_adamw_read_moments",
+    "st_quantize_rows", "st_int8_matmul", "st_set_frozen_features_int8",
     "st_adamw_write_moments", "st_adamw_step_count", "st_adamw_destroy", "st_adamw_last_error",
 ]
 ST_NOALLOC_MAX_CLASSES = 64
@@ -155,6 +156,12 @@ def load_library() -> ctypes.CDLL:
     lib.st_agreement_noalloc.argtypes = [vp, vp, i64, i32, vp, vp, vp]
     lib.st_measure_arithmetic_peaks.restype = ctypes.c_int
     lib.st_measure_arithmetic_peaks.argtypes = [vp, ctypes.POINTER(dbl), ctypes.POINTER(dbl)]
+    lib.st_quantize_rows.restype = ctypes.c_int
+    lib.st_quantize_rows.argtypes = [vp, i32, i64, i64, i64, i64, vp, i64, vp, vp]
+    lib.st_int8_matmul.restype = ctypes.c_int
+    lib.st_int8_matmul.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, i64, i64, i64, vp, i32, i64, vp]
+    lib.st_set_frozen_features_int8.restype = ctypes.c_int
+    lib.st_set_frozen_features_int8.argtypes = [vp, i32, vp, i64, vp, vp, i64, vp, vp, i32, i64]
     lib.st_adamw_create.restype = ctypes.c_int
     lib.st_adamw_create.argtypes = [ctypes.POINTER(st_adamw_desc), ctypes.POINTER(st_adamw_tensor), ctypes.POINTER(vp)]
     lib.st_adamw_set_grads.restype = ctypes.c_int
@@ -418,6 +425,57 @@ def st_measure_arithmetic_peaks(cuda_stream: int = 0):
     _status_only(load_library().st_measure_arithmetic_peaks(cuda_stream or None, ctypes.byref(fma), ctypes.byref(ex2)),
                  "st_measure_arithmetic_peaks")
     return fma.value, ex2.value
+
+
+# ---------------------------------------------------------------------------- 8-bit integer layers of the frozen part
+def _matrix(t, names, what: str):
+    """(address, element type's name, rows, columns, row pitch) of a CUDA matrix whose rows are contiguous."""
+    name = str(t.dtype).removeprefix("torch.")
+    if name not in names:
+        raise TypeError(f"{what}: need {' or '.join(names)}, got {t.dtype}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError(f"{what}: need a matrix whose rows are contiguous, got shape {tuple(t.shape)} with strides {t.stride()}")
+    rows, cols = t.shape
+    return t.data_ptr(), name, rows, cols, t.stride(0) if rows > 1 else max(cols, 1)
+
+
+def st_quantize_rows(x, q, scale, cuda_stream: int = 0) -> None:
+    """Rows of `x` (CUDA matrix of any strides; float32, bfloat16 or float16) to int8 `q` (rows contiguous) with one scale each.
+    The pixels of a planar feature map are the rows of `features.view(channels, -1).t()`."""
+    name = _dtype_name(x, "x")
+    if x.dim() != 2:
+        raise TypeError(f"x: need a matrix, got shape {tuple(x.shape)}")
+    address, _, rows, cols, ldq = _matrix(q, ("int8",), "q")
+    if (rows, cols) != tuple(x.shape):
+        raise ValueError(f"q: shape {(rows, cols)}, need {tuple(x.shape)}")
+    _check(load_library().st_quantize_rows(x.data_ptr(), _TYPE_OF[name], rows, cols, x.stride(0), x.stride(1), address, ldq,
+                                           _ptr(scale, "float32", rows, "scale"), cuda_stream or None), None)
+
+
+def _int8_operands(x, x_scale, w, w_scale, bias):
+    xa, _, m, k, ldx = _matrix(x, ("int8",), "x")
+    wa, _, n, kw, ldw = _matrix(w, ("int8",), "w")
+    if k != kw:
+        raise ValueError(f"w: {kw} columns, x has {k}")
+    return (xa, ldx, _ptr(x_scale, "float32", m, "x_scale"), wa, ldw, _ptr(w_scale, "float32", n, "w_scale"), _ptr(bias, "float32", n, "bias")), m, n, k
+
+
+def st_int8_matmul(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, cuda_stream: int = 0) -> None:
+    """y[m][n] = act((sum_k x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n]); x, w int8 and y float32, bfloat16 or float16, CUDA matrices
+    whose rows are contiguous (rows of x and w at multiples of 16 bytes run on tensor cores)."""
+    operands, m, n, k = _int8_operands(x, x_scale, w, w_scale, bias)
+    ya, name, my, ny, ldy = _matrix(y, tuple(_TYPE_OF), "y")
+    if (my, ny) != (m, n):
+        raise ValueError(f"y: shape {(my, ny)}, need {(m, n)}")
+    _check(load_library().st_int8_matmul(*operands, int(relu), m, n, k, ya, _TYPE_OF[name], ldy, cuda_stream or None), None)
+
+
+def st_set_frozen_features_int8(ctx: _Ctx, stream: int, x, x_scale, w, w_scale, bias=None, relu: bool = False) -> None:
+    """The frozen part's last pointwise layer in 8 bits into the stream's feature cache (x: a pixel per row, w: c_in rows)."""
+    operands, m, n, k = _int8_operands(x, x_scale, w, w_scale, bias)
+    if m != ctx.p or n != ctx.c_in:
+        raise ValueError(f"x and w: {m} pixels and {n} channels, need {ctx.p} and {ctx.c_in}")
+    _check(load_library().st_set_frozen_features_int8(ctx.handle, stream, *operands, int(relu), k), ctx)
 
 
 # ---------------------------------------------------------------------------- the optimiser of tensors outside a context

@@ -1,0 +1,360 @@
+// st_int8_matmul — product of 8-bit integers with a scale per token (row of x) and per output channel (row of w):
+//   y[m][n] = act((sum_k x[m][k] w[n][k]) sx[m] sw[n] + b[n])
+// Sums are exact in 32-bit integers; the four fp32 operations behind them are rounded one by one, in the order above.
+//
+// Both operands are K-major, so TMA's 128-byte-swizzled tiles go into tcgen05.mma kind::i8 (K = 32 bytes an instruction) as they
+// are; extents that are no multiples of a tile are TMA's zero fill.  Three forms:
+//   int8_tiles_kernel   many tokens: tokens are the accumulator's lanes, up to 256 channels its columns; a persistent block per SM, ring of
+//                       128-byte slices of K, two accumulators so that one is scaled and stored while the other is summed.
+//   int8_split_kernel   few tokens, or too few tiles for the SMs: channels are the lanes, up to 128 tokens the columns; the blocks of a
+//                       cluster share a tile's K range and add their sums through distributed shared memory.
+//   int8_plain_kernel   operands that TMA cannot read (bases or pitches that are no multiples of 16 bytes): dp4a.
+#include "../../include/shadowtutor.h"
+#include "st_internal.h"
+#include "int8_common.h"
+#include "tc_common.cuh"
+
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cstdlib>
+#include <mutex>
+
+namespace st {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kTile = 128;                      // lanes of an accumulator
+constexpr int kSlice = 128;                     // bytes of K in a stage: one swizzled row
+constexpr int kSmemAlign = 1024;
+
+// Instruction descriptor of tcgen05.mma kind::i8: D format 2 (s32), A and B format 1 (s8), both K-major
+__host__ __device__ constexpr uint32_t instr_desc_i8(int M, int N)
+{
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+struct Out {
+    void* y; int64_t ldy; int type, wide;       // wide: rows of y take whole 16-byte stores
+    const float *sx, *sw, *bias; int relu;
+    int M, N;
+};
+__device__ __forceinline__ float finish(int acc, float sx, float sw, float bias, bool has_bias, int relu)
+{
+    float y = __fmul_rn(__fmul_rn((float)acc, sx), sw);
+    if (has_bias) y = __fadd_rn(y, bias);
+    return relu ? (y < 0.f ? 0.f : y) : y;      // NaN (a token or channel that is not finite) stays NaN
+}
+__device__ __forceinline__ uint16_t round16(float y, int type)
+{
+    return type == ST_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
+}
+__device__ __forceinline__ uint32_t round16x2(float lo, float hi, int type)
+{
+    if (type == ST_BF16) { const __nv_bfloat162 q = __floats2bfloat162_rn(lo, hi); return *(const uint32_t*)&q; }
+    const __half2 q = __floats2half2_rn(lo, hi);
+    return *(const uint32_t*)&q;
+}
+__device__ __forceinline__ void put_one(const Out& o, int64_t at, float y)
+{
+    if (o.type == ST_F32) ((float*)o.y)[at] = y;
+    else ((uint16_t*)o.y)[at] = round16(y, o.type);
+}
+
+// ---- many tokens ------------------------------------------------------------------------------------------------
+constexpr int kTilesThreads = 384;              // producer, issuer, two idle warps (registers), eight that store
+// `stall`: 0; a test of the give-up path makes the first stage expect bytes that no copy delivers, so that the waits behind it run out
+struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices; unsigned int* err; uint32_t stall; };
+
+template <int BN>
+struct TilesShape {
+    static constexpr int stage_bytes = (kTile + BN) * kSlice, stages = (int)(200 * 1024 / stage_bytes) < 8 ? (int)(200 * 1024 / stage_bytes) : 8;
+    static constexpr size_t bytes = (size_t)stages * stage_bytes + kSmemAlign;
+    static constexpr int acc_cols = BN < 32 ? 32 : BN;
+};
+
+template <int BN>
+__global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const TilesArgs a)
+{
+    using Shape = TilesShape<BN>;
+    constexpr int S = Shape::stages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t ring = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1);
+    __shared__ __align__(8) uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ float column[2][2][BN];          // per accumulator: scales and bias of its columns
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), 2 * Shape::acc_cols);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 8); }
+        fence_barrier_init();
+        prefetch_map(&tm_x); prefetch_map(&tm_w);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tiles = a.m_tiles * a.n_tiles;
+    bool ok = true;
+    if (warp == 0) {                            // producer
+        uint32_t stage = 0, phase = 1;          // a fresh barrier's phase before the first counts as completed
+        for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
+            for (int s = 0; s < a.slices; ++s) {
+                ok = mbar_wait(smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * Shape::stage_bytes;
+                    mbar_expect_tx(bar, (a.tile_m + BN) * kSlice + (t == (int)blockIdx.x && s == 0 ? a.stall : 0u));
+                    tma_load_2d(dst, &tm_x, bar, s * kSlice, m0);
+                    tma_load_2d(dst + kTile * kSlice, &tm_w, bar, s * kSlice, n0);
+                }
+                __syncwarp();
+                if (++stage == S) { stage = 0; phase ^= 1; }
+            }
+        }
+    } else if (warp == 1) {                     // issuer
+        constexpr uint32_t idesc = instr_desc_i8(kTile, BN);
+        uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 1;
+        for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            ok = mbar_wait(smem_u32(&acc_empty[acc]), acc_phase, a.err, kWaitDone);
+            if (!ok) break;
+            tc_fence_after_sync();
+            for (int s = 0; s < a.slices; ++s) {
+                ok = mbar_wait(smem_u32(&full[stage]), phase, a.err, kWaitFull);
+                if (!ok) break;
+                tc_fence_after_sync();
+                if (elect_one()) {
+                    const uint32_t src = ring + stage * Shape::stage_bytes;
+                    const uint64_t da = smem_desc(src, 16, 1024), db = smem_desc(src + kTile * kSlice, 16, 1024);
+#pragma unroll
+                    for (int k = 0; k < kSlice / 32; ++k) umma_i8(tmem + acc * Shape::acc_cols, da + 2 * k, db + 2 * k, idesc, (s | k) != 0);
+                    umma_commit(smem_u32(&empty[stage]));
+                    if (s == a.slices - 1) umma_commit(smem_u32(&acc_full[acc]));
+                }
+                __syncwarp();
+                if (++stage == S) { stage = 0; phase ^= 1; }
+            }
+            if (acc) acc_phase ^= 1;
+            acc ^= 1;
+        }
+    } else if (warp >= 4) {                     // scale and store: warps 4..7 the lower half of the columns, 8..11 the upper
+        const int half = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * half;
+        const Out& o = a.out;
+        uint32_t acc = 0, acc_phase = 0;
+        for (int t = (int)blockIdx.x; t < tiles; t += gridDim.x) {
+            const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
+            const int64_t row = (int64_t)m0 + quarter * 32 + lane;
+            const bool mine = quarter * 32 + lane < a.tile_m && row < o.M;
+            const float sx = mine ? o.sx[row] : 0.f;
+            for (int c = half * (BN / 2) + tid; c < (half + 1) * (BN / 2); c += 128) {
+                const bool in = n0 + c < o.N;
+                column[acc][0][c] = in ? o.sw[n0 + c] : 0.f;
+                column[acc][1][c] = in && o.bias ? o.bias[n0 + c] : 0.f;
+            }
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+            // a warp whose wait has given up goes on through the tiles without storing: the others wait for it above
+            if (ok) ok = mbar_wait(smem_u32(&acc_full[acc]), acc_phase, a.err, kWaitDone);
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int c0 = half * (BN / 2); ok && c0 < (half + 1) * (BN / 2) && n0 + c0 < o.N; c0 += 32) {
+                float v[32];
+                __syncwarp();
+                tmem_ld_32x32(tmem + acc * Shape::acc_cols + ((uint32_t)(quarter * 32) << 16) + c0, v);
+                if (!mine) continue;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = finish(__float_as_int(v[j]), sx, column[acc][0][c0 + j], column[acc][1][c0 + j], o.bias != nullptr, o.relu);
+                const int64_t at = row * o.ldy + n0 + c0;
+                if (o.wide && n0 + c0 + 32 <= o.N) {
+                    if (o.type == ST_F32) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) *(float4*)((float*)o.y + at + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            *(uint4*)((uint16_t*)o.y + at + j) = make_uint4(round16x2(v[j], v[j + 1], o.type), round16x2(v[j + 2], v[j + 3], o.type),
+                                                                           round16x2(v[j + 4], v[j + 5], o.type), round16x2(v[j + 6], v[j + 7], o.type));
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (n0 + c0 + j < o.N) put_one(o, at + j, v[j]);
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
+            if (acc) acc_phase ^= 1;
+            acc ^= 1;
+        }
+    }
+    if (!ok) drain_after_error();
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 2) tmem_dealloc(tmem, 2 * Shape::acc_cols);
+}
+
+// ---- operands at any address ----------------------------------------------------------------------------------------
+constexpr int kPlainTile = 64, kPlainK = 64, kPlainPitch = kPlainK / 4 + 1;
+__global__ void __launch_bounds__(256) int8_plain_kernel(const int8_t* __restrict__ x, int64_t ldx, const int8_t* __restrict__ w, int64_t ldw, int K, const Out o)
+{
+    __shared__ uint32_t xs[kPlainTile * kPlainPitch], ws[kPlainTile * kPlainPitch];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t m0 = (int64_t)blockIdx.x * kPlainTile;
+    const int n0 = blockIdx.y * kPlainTile, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    int acc[4][4] = {};
+    for (int k0 = 0; k0 < K; k0 += kPlainK) {
+        for (int i = threadIdx.x; i < kPlainTile * kPlainK; i += 256) {
+            const int r = i / kPlainK, c = i % kPlainK;
+            const bool k_in = k0 + c < K;
+            ((int8_t*)xs)[r * kPlainPitch * 4 + c] = k_in && m0 + r < o.M ? x[(m0 + r) * ldx + k0 + c] : (int8_t)0;
+            ((int8_t*)ws)[r * kPlainPitch * 4 + c] = k_in && n0 + r < o.N ? w[(int64_t)(n0 + r) * ldw + k0 + c] : (int8_t)0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlainK / 4; ++k) {
+            uint32_t a[4], b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { a[i] = xs[(ty + 16 * i) * kPlainPitch + k]; b[i] = ws[(tx + 16 * i) * kPlainPitch + k]; }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a((int)a[i], (int)b[j], acc[i][j]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t m = m0 + ty + 16 * i;
+        if (m >= o.M) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int n = n0 + tx + 16 * j;
+            if (n < o.N) put_one(o, m * o.ldy + n, finish(acc[i][j], o.sx[m], o.sw[n], o.bias ? o.bias[n] : 0.f, o.bias != nullptr, o.relu));
+        }
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+// What a device needs before its first launch: the kernels' limits of shared memory, and a word in pinned host memory in which a wait that gave up
+// leaves its code, so that the next call can tell without waiting for the device.
+struct Device { bool ready = false; int sms = 0; unsigned int *err = nullptr, *err_dev = nullptr; };
+constexpr int kMaxDevices = 64;
+Device g_devices[kMaxDevices];
+std::mutex g_mutex;
+
+cudaError_t device_for(int index, Device** out)
+{
+    if (index < 0 || index >= kMaxDevices) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(g_mutex);
+    Device& d = g_devices[index];
+    *out = &d;
+    if (d.ready) return cudaSuccess;
+    cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, index);
+    for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>})
+        if (e == cudaSuccess) e = allow_shared_memory(k);
+    if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
+    if (e == cudaSuccess) { *d.err = 0; e = cudaHostGetDevicePointer((void**)&d.err_dev, d.err, 0); }
+    d.ready = e == cudaSuccess;
+    return e;
+}
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+uint32_t stall_bytes()
+{
+    const char* e = getenv("ST_TEST_STALL_INT8");
+    return e && e[0] == '1' ? 16u : 0u;
+}
+
+bool operand_map(CUtensorMap* m, const int8_t* q, int64_t rows, int64_t ld, int64_t K, int box_rows, char* msg, size_t msg_len, const char* what)
+{
+    const uint64_t dims[2] = {(uint64_t)K, (uint64_t)rows}, strides[1] = {(uint64_t)(rows == 1 ? (K + 15) / 16 * 16 : ld)};
+    const uint32_t box[2] = {kSlice, (uint32_t)box_rows};
+    return encode_tensor_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, q, 2, dims, strides, box, msg, msg_len, what);
+}
+
+}  // namespace
+
+int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
+{
+    const auto cuda_fail = [](cudaError_t e) { cudaGetLastError(); return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", cudaGetErrorString(e)); };
+    int index = 0;
+    Device* d = nullptr;
+    cudaError_t e = cudaGetDevice(&index);
+    if (e == cudaSuccess) e = device_for(index, &d);
+    if (e != cudaSuccess) return cuda_fail(e);
+    if (const unsigned int code = *(volatile unsigned int*)d->err) {
+        *(volatile unsigned int*)d->err = 0;
+        return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of an earlier product gave up (code %u); its result is not complete", code);
+    }
+    Out o = {p.y, p.ldy, p.y_type, 0, p.x_scale, p.w_scale, p.bias, p.relu, (int)p.M, (int)p.N};
+    const int64_t size = p.y_type == ST_F32 ? 4 : 2;
+    o.wide = aligned(p.y, 16) && (p.M == 1 || p.ldy * size % 16 == 0);
+    const bool tma = aligned(p.x, 16) && aligned(p.w, 16) && (p.M == 1 || p.ldx % 16 == 0) && (p.N == 1 || p.ldw % 16 == 0);
+    if (!tma) {
+        const dim3 grid((unsigned)((p.M + kPlainTile - 1) / kPlainTile), (unsigned)((p.N + kPlainTile - 1) / kPlainTile));
+        e = launch_early(pdl_enabled(), int8_plain_kernel, grid, dim3(256), 0, s, p.x, p.ldx, p.w, p.ldw, (int)p.K, o);
+        return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
+    }
+    char msg[160] = "";
+    CUtensorMap tx, tw;
+    const int bn = p.N <= 64 ? 64 : p.N <= 128 ? 128 : 256;
+    TilesArgs a;
+    a.out = o; a.tile_m = kTile; a.m_tiles = (int)((p.M + kTile - 1) / kTile); a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = (int)((p.K + kSlice - 1) / kSlice);
+    a.err = d->err_dev;
+    a.stall = stall_bytes();
+    if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, bn, msg, sizeof msg, "w"))
+        return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
+    const dim3 grid((unsigned)std::min<int64_t>((int64_t)a.m_tiles * a.n_tiles, d->sms));
+    const auto go = [&](auto kernel, size_t bytes) { return launch_early(pdl_enabled(), kernel, grid, dim3(kTilesThreads), bytes, s, tx, tw, a); };
+    e = bn == 64 ? go(int8_tiles_kernel<64>, TilesShape<64>::bytes) : bn == 128 ? go(int8_tiles_kernel<128>, TilesShape<128>::bytes)
+                                                                               : go(int8_tiles_kernel<256>, TilesShape<256>::bytes);
+    return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
+}
+
+}  // namespace st
+
+using namespace st;
+
+extern "C" st_status st_int8_matmul(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale,
+                                    const float* bias, int32_t relu, int64_t M, int64_t N, int64_t K, void* y, int32_t y_type, int64_t ldy, void* cuda_stream)
+{
+    const auto bad = [](const char* what) { return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_int8_matmul: %s", what); };
+    if (M < 0 || N < 0 || K < 1) return bad("needs M >= 0, N >= 0 and K >= 1");
+    if (y_type != ST_F32 && y_type != ST_BF16 && y_type != ST_F16) return bad("y_type is not an st_dtype");
+    if (relu & ~1) return bad("relu must be 0 or 1");
+    if (ldx < K || ldw < K || ldy < N) return bad("ldx, ldw below K or ldy below N");
+    if (K > kMaxInt8K) return (st_status)fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: K above %d could overflow the 32-bit sums", kMaxInt8K);
+    if (M > kMaxInt8Extent - 255 || N > kMaxInt8N || !extent_fits(M, ldx, K, 1) || !extent_fits(N, ldw, K, 1) || !extent_fits(M, ldy, N, 1) ||
+        ((M + 127) / 128) * ((N + 63) / 64) > kMaxInt8Extent)
+        return (st_status)fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: extents beyond the kernels' 32-bit counts of tiles");
+    if (M == 0 || N == 0) return ST_OK;
+    Int8Buffers b("st_int8_matmul");
+    b.add("x", x, 1, (M - 1) * ldx + K, false);
+    b.add("x_scale", x_scale, 4, M, false);
+    b.add("w", w, 1, (N - 1) * ldw + K, false);
+    b.add("w_scale", w_scale, 4, N, false);
+    if (bias) b.add("bias", bias, 4, N, false);
+    b.add("y", y, y_type == ST_F32 ? 4 : 2, (M - 1) * ldy + N, true);
+    if (!b.ok()) return b.status();
+    const Int8Product p = {x, ldx, x_scale, w, ldw, w_scale, bias, relu, M, N, K, y, y_type, ldy};
+    return (st_status)launch_int8_matmul(p, (cudaStream_t)cuda_stream);
+}

@@ -867,6 +867,23 @@ st_status st_set_frozen_features(st_ctx* ctx, int32_t stream, const float* feat_
     return ST_OK;
 }
 
+st_status st_set_frozen_features_int8(st_ctx* ctx, int32_t stream, const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                                      const float* w_scale, const float* bias, int32_t relu, int64_t K)
+{
+    st_status st = check_stream_index(ctx, stream);
+    if (st != ST_OK) return st;
+    if (!ctx->bf16_mode) return fail(ctx, ST_ERR_UNSUPPORTED, "st_set_frozen_features_int8: needs gemm_precision 1");
+    st = st_int8_matmul(x, ldx, x_scale, w, ldw, w_scale, bias, relu, ctx->p, ctx->Cin, K, ctx->x_bf16 + (int64_t)stream * ctx->p * ctx->Cin, ST_BF16,
+                        ctx->Cin, ctx->stream);
+    if (st != ST_OK) return fail(ctx, st, "st_set_frozen_features_int8: %s", st_last_error(nullptr));
+    ctx->launches += 1;
+    ctx->has_feat[stream] = 1;
+    ctx->settled = false;
+    ctx->z_current = false;
+    ctx->prefix_current = false;
+    return ST_OK;
+}
+
 st_status st_set_skip_features(st_ctx* ctx, int32_t stream, int32_t block, const float* feat_chw)
 {
     st_status st = check_stream_index(ctx, stream);

@@ -190,6 +190,16 @@ bool student_mask_fused_supported(int C);   // confusion counters fit shared mem
 cudaError_t prepare_student_mask();         // once per device, outside any stream capture
 void launch_student_mask(const StudentMaskArgs& a, cudaStream_t s);
 
+// ---- 8-bit integer products (k_int8.cu): arguments checked by the entry points; returns an st_status, the text as fail_on_thread
+struct Int8Product {
+    const int8_t* x; int64_t ldx; const float* x_scale;
+    const int8_t* w; int64_t ldw; const float* w_scale;
+    const float* bias; int relu;
+    int64_t M, N, K;
+    void* y; int y_type; int64_t ldy;
+};
+int launch_int8_matmul(const Int8Product& p, cudaStream_t s);
+
 // ---- fp32 CUDA-core convolutions (gemm_precision 0) -------------------------------------------
 // Planes [C][rows][pitch] with the map at row kPadTop, column kPadLeft and zeros around it (allocated zero; every writer
 // touches the interior only).  Rows start on 16-byte boundaries at any width and reach past the last 32 x 4 pixel tile.
