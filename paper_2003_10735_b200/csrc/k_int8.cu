@@ -81,7 +81,7 @@ struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices; unsigned int* 
 
 template <int BN>
 struct TilesShape {
-    static constexpr int stage_bytes = (kTile + BN) * kSlice, stages = (int)(200 * 1024 / stage_bytes) < 8 ? (int)(200 * 1024 / stage_bytes) : 8;
+    static constexpr int stage_bytes = (kTile + BN) * kSlice, stages = (int)(192 * 1024 / stage_bytes) < 8 ? (int)(192 * 1024 / stage_bytes) : 8;
     static constexpr size_t bytes = (size_t)stages * stage_bytes + kSmemAlign;
     static constexpr int acc_cols = BN < 32 ? 32 : BN;
 };
@@ -95,6 +95,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     const uint32_t ring = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1);
     __shared__ __align__(8) uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
+    __shared__ float turned[8][32 * 17];
     __shared__ float column[2][2][BN];          // per accumulator: scales and bias of its columns
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), 2 * Shape::acc_cols);
@@ -177,11 +178,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
                 float v[32];
                 __syncwarp();
                 tmem_ld_32x32(tmem + acc * Shape::acc_cols + ((uint32_t)(quarter * 32) << 16) + c0, v);
-                if (!mine) continue;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = finish(__float_as_int(v[j]), sx, column[acc][0][c0 + j], column[acc][1][c0 + j], o.bias != nullptr, o.relu);
                 const int64_t at = row * o.ldy + n0 + c0;
                 if (o.wide && n0 + c0 + 32 <= o.N) {
+                    if (!mine) continue;
                     if (o.type == ST_F32) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) *(float4*)((float*)o.y + at + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
@@ -192,9 +193,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
                                                                            round16x2(v[j + 4], v[j + 5], o.type), round16x2(v[j + 6], v[j + 7], o.type));
                     }
                 } else {
+                    // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
+                    // 157 us with each lane storing its own row value by value)
+                    float* piece = turned[warp - 4];
+                    const int rows_in = min(min(a.tile_m, o.M - m0) - quarter * 32, 32), r0 = lane / 16, c = lane % 16;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (n0 + c0 + j < o.N) put_one(o, at + j, v[j]);
+                    for (int h = 0; h < 32; h += 16) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) piece[lane * 17 + j] = v[h + j];
+                        __syncwarp();
+                        const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0 + h + c;
+                        if (n0 + c0 + h + c < o.N)
+#pragma unroll 4
+                            for (int r = r0; r < rows_in; r += 2) put_one(o, first + r * o.ldy, piece[r * 17 + c]);
+                        __syncwarp();
+                    }
                 }
             }
             tc_fence_before_sync();
@@ -208,6 +221,129 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     tc_fence_before_sync();
     __syncthreads();
     if (warp == 2) tmem_dealloc(tmem, 2 * Shape::acc_cols);
+}
+
+// ---- few tokens, or few tiles --------------------------------------------------------------------------------------
+constexpr int kSplitThreads = 192;              // four warps that store, producer, issuer
+constexpr int kMaxSplitStages = 8;
+struct SplitArgs { Out out; int slices, splits, stages; unsigned int* err; uint32_t stall; };
+
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ int load_cluster(uint32_t addr, uint32_t rank)
+{
+    uint32_t at; int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// Block r of a cluster of `splits` sums slices [r, r + 1) / splits of K for 128 channels x BT tokens; sums are whole numbers, so their order does not
+// matter.  Token t of the tile is then added up over the blocks, scaled and stored by block t % splits.
+template <int BT>
+__global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const SplitArgs a)
+{
+    constexpr int kStage = (kTile + BT) * kSlice, kCols = BT < 32 ? 32 : BT;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t ring = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1);
+    __shared__ __align__(8) uint64_t full[kMaxSplitStages], empty[kMaxSplitStages], acc_full;
+    __shared__ uint32_t tmem_slot;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (warp == 0) tmem_alloc(smem_u32(&tmem_slot), kCols);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+        mbar_init(smem_u32(&acc_full), 1);
+        fence_barrier_init();
+        prefetch_map(&tm_x); prefetch_map(&tm_w);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    const int split = blockIdx.x % a.splits, n0 = blockIdx.x / a.splits * kTile, m0 = blockIdx.y * BT;
+    const int begin = (int)((int64_t)a.slices * split / a.splits), end = (int)((int64_t)a.slices * (split + 1) / a.splits);
+    const Out& o = a.out;
+    pdl_wait();
+    pdl_launch_dependents();
+    bool ok = true;
+    const int count = min(o.M - m0, BT);        // tokens of the tile
+    if (warp == 4) {
+        uint32_t stage = 0, phase = 1;
+        for (int s = begin; s < end; ++s) {
+            ok = mbar_wait(smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * kStage;
+                mbar_expect_tx(bar, kStage + (s == begin ? a.stall : 0u));
+                tma_load_2d(dst, &tm_w, bar, s * kSlice, n0);
+                tma_load_2d(dst + kTile * kSlice, &tm_x, bar, s * kSlice, m0);
+            }
+            __syncwarp();
+            if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+        }
+    } else if (warp == 5) {
+        constexpr uint32_t idesc = instr_desc_i8(kTile, BT);
+        uint32_t stage = 0, phase = 0;
+        for (int s = begin; s < end; ++s) {
+            ok = mbar_wait(smem_u32(&full[stage]), phase, a.err, kWaitFull);
+            if (!ok) break;
+            tc_fence_after_sync();
+            if (elect_one()) {
+                const uint32_t src = ring + stage * kStage;
+                const uint64_t da = smem_desc(src, 16, 1024), db = smem_desc(src + kTile * kSlice, 16, 1024);
+#pragma unroll
+                for (int k = 0; k < kSlice / 32; ++k) umma_i8(tmem, da + 2 * k, db + 2 * k, idesc, (s != begin) | (k != 0));
+                umma_commit(smem_u32(s == end - 1 ? &acc_full : &empty[stage]));
+            }
+            __syncwarp();
+            if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+        }
+    } else if (warp < 4) {
+        const int channel = n0 + threadIdx.x;
+        const bool mine = channel < o.N;
+        const float sw = mine ? o.sw[channel] : 0.f, bias = mine && o.bias ? o.bias[channel] : 0.f;
+        ok = mbar_wait(smem_u32(&acc_full), 0, a.err, kWaitDone);
+        tc_fence_after_sync();
+        if (ok) {
+#pragma unroll
+            for (int c0 = 0; c0 < BT; c0 += 16) {
+                if (c0 >= count) break;
+                float v[16];
+                __syncwarp();
+                tmem_ld_32x16(tmem + ((uint32_t)(warp * 32) << 16) + c0, v);
+                if (a.splits == 1) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (mine && c0 + j < count) put_one(o, (int64_t)(m0 + c0 + j) * o.ldy + channel, finish(__float_as_int(v[j]), o.sx[m0 + c0 + j], sw, bias, o.bias != nullptr, o.relu));
+                } else {                        // every MMA has read its operands: the ring is free
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c0 + j < count) asm volatile("st.shared.b32 [%0], %1;" ::"r"(ring + ((c0 + j) * kTile + threadIdx.x) * 4), "r"(__float_as_int(v[j])) : "memory");
+                }
+            }
+        }
+    }
+    if (!ok) drain_after_error();
+    __syncwarp();
+    if (a.splits > 1) {
+        const int all_ok = __syncthreads_and(ok);
+        cluster_sync();
+        if (warp < 4 && all_ok) {
+            const int channel = n0 + threadIdx.x;
+            const bool mine = channel < o.N;
+            const float sw = mine ? o.sw[channel] : 0.f, bias = mine && o.bias ? o.bias[channel] : 0.f;
+            for (int c = split; c < count; c += a.splits) {
+                int sum = 0;
+                const uint32_t at = ring + (c * kTile + threadIdx.x) * 4;
+                for (int r = 0; r < a.splits; ++r) sum += load_cluster(at, r);
+                if (mine) put_one(o, (int64_t)(m0 + c) * o.ldy + channel, finish(sum, o.sx[m0 + c], sw, bias, o.bias != nullptr, o.relu));
+            }
+        }
+        __syncwarp();
+        cluster_sync();                         // nobody leaves while others read its sums
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tmem, kCols);
 }
 
 // ---- operands at any address ----------------------------------------------------------------------------------------
@@ -268,7 +404,8 @@ cudaError_t device_for(int index, Device** out)
     *out = &d;
     if (d.ready) return cudaSuccess;
     cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, index);
-    for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>})
+    for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>,
+                          (const void*)int8_split_kernel<16>, (const void*)int8_split_kernel<32>, (const void*)int8_split_kernel<64>, (const void*)int8_split_kernel<128>})
         if (e == cudaSuccess) e = allow_shared_memory(k);
     if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
     if (e == cudaSuccess) { *d.err = 0; e = cudaHostGetDevicePointer((void**)&d.err_dev, d.err, 0); }
@@ -316,9 +453,36 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     }
     char msg[160] = "";
     CUtensorMap tx, tw;
+    const int slices = (int)((p.K + kSlice - 1) / kSlice);
+    const char* form = getenv("ST_INT8_FORM");
+    if (form ? form[0] == 's' : p.M <= 128) {
+        const int bt = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+        const int64_t m_tiles = (p.M + bt - 1) / bt, n_tiles = (p.N + kTile - 1) / kTile;
+        int splits = 1;
+        while (splits < 8 && m_tiles * n_tiles * splits * 2 <= d->sms + 20 && slices >= splits * 2) splits *= 2;
+        if (form && form[1]) splits = form[1] - '0';
+        SplitArgs a;
+        a.out = o; a.slices = slices; a.splits = splits; a.err = d->err_dev; a.stall = stall_bytes();
+        const int stage = (kTile + bt) * kSlice, per = (slices + splits - 1) / splits;
+        a.stages = std::min({kMaxSplitStages, per, 200 * 1024 / stage});
+        const size_t bytes = (size_t)std::max(a.stages * stage, splits > 1 ? bt * kTile * 4 : 0) + kSmemAlign;
+        if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, bt, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, kTile, msg, sizeof msg, "w"))
+            return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(n_tiles * splits), (unsigned)m_tiles); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = bytes; cfg.stream = s;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)splits; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at; cfg.numAttrs = pdl_enabled() ? 2 : 1;
+        e = bt == 16 ? cudaLaunchKernelEx(&cfg, int8_split_kernel<16>, tx, tw, a) : bt == 32 ? cudaLaunchKernelEx(&cfg, int8_split_kernel<32>, tx, tw, a)
+          : bt == 64 ? cudaLaunchKernelEx(&cfg, int8_split_kernel<64>, tx, tw, a) : cudaLaunchKernelEx(&cfg, int8_split_kernel<128>, tx, tw, a);
+        return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
+    }
     const int bn = p.N <= 64 ? 64 : p.N <= 128 ? 128 : 256;
     TilesArgs a;
-    a.out = o; a.tile_m = kTile; a.m_tiles = (int)((p.M + kTile - 1) / kTile); a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = (int)((p.K + kSlice - 1) / kSlice);
+    a.out = o; a.tile_m = kTile; a.m_tiles = (int)((p.M + kTile - 1) / kTile); a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices;
     a.err = d->err_dev;
     a.stall = stall_bytes();
     if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, bn, msg, sizeof msg, "w"))

@@ -6,9 +6,9 @@
 //   other strides (planar feature maps, whose rows are pixels): a block takes 32 rows and reads them channel by channel, a row to a
 //     lane, so that planes are read in whole sectors; the integers are turned round in shared memory
 //
-// The quotient is x * (1 / scale) with the approximate reciprocal; it is off by at most 127 * 1.5 * 2^-23 of a step, so it gives the whole number
-// unless it lies within kNear of a half.  There (one value in 5000) the quotient in double decides: of two fp32 numbers it is either a
-// half exactly or at least 2^-32 away from one.
+// The quotient is x * (1 / scale), off by at most 127 * 2^-23 of a step (1.5e-5), so it gives the whole number unless it lies within kNear
+// of a half.  There (one value in 25000; a lane then takes all values of its piece that way) the quotient in double decides: of two fp32
+// numbers it is either a half exactly or at least 2^-32 away from one.
 #include "../../include/shadowtutor.h"
 #include "st_internal.h"
 #include "int8_common.h"
@@ -22,34 +22,46 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr float kRound = 12582912.f;            // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
-constexpr float kNear = 1e-4f;
+constexpr float kNear = 2e-5f;
 constexpr float kLeastScale = 0x1p-100f;        // below it every quotient is formed in double
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 
-struct RowScale { float scale, inverse; bool exact; };
+// `doubt`: added to a value's distance from the whole numbers; 1 sends every value through the quotient in double.  `mask`: 0 makes all integers 0.
+struct RowScale { float scale, inverse, doubt; uint32_t mask; };
 // From the bits of the row's largest |x| (NaN lies above infinity).  A row that is not finite has scale NaN and integers 0.
 __device__ __forceinline__ RowScale row_scale(uint32_t top)
 {
     RowScale r;
-    if (top >= 0x7f800000u) { r.scale = __uint_as_float(0x7fffffffu); r.inverse = 0.f; r.exact = false; return r; }
-    r.scale = __fdiv_rn(__uint_as_float(top), 127.f);
-    r.exact = r.scale < kLeastScale && r.scale > 0.f;
-    r.inverse = r.scale < kLeastScale ? 0.f : __frcp_rn(r.scale);
+    const bool finite = top < 0x7f800000u;
+    r.scale = finite ? __fdiv_rn(__uint_as_float(top), 127.f) : __uint_as_float(0x7fffffffu);
+    r.doubt = r.scale < kLeastScale && r.scale > 0.f ? 1.f : 0.f;
+    r.inverse = r.scale >= kLeastScale ? __frcp_rn(r.scale) : 0.f;
+    r.mask = finite ? 0xffffffffu : 0u;
     return r;
 }
-// the integer in the low byte
-__device__ __forceinline__ uint32_t quantized(float x, const RowScale& r)
+__device__ __noinline__ uint32_t exact_quotient(float x, float scale)
 {
-    if (r.scale != r.scale) return 0u;
-    const float t = x * r.inverse, y = t + kRound;
-    if (fabsf(t - (y - kRound)) > 0.5f - kNear || r.exact) {
-        const double q = rint((double)x / (double)r.scale);
-        return (uint32_t)(int)fmin(fmax(q, -127.0), 127.0);
+    const double q = rint((double)x / (double)scale);
+    return (uint32_t)(int)fmin(fmax(q, -127.0), 127.0);
+}
+__device__ __forceinline__ uint32_t low_bytes(const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0040u), __byte_perm(c[2], c[3], 0x0040u), 0x5410u); }
+// the integers of V values in the low bytes of words
+template <int V>
+__device__ __forceinline__ void quantized(uint32_t (&b)[V], const float (&x)[V], const RowScale& r)
+{
+    float far = r.doubt;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const float t = x[j] * r.inverse, y = t + kRound;
+        far = fmaxf(far, fabsf(t - (y - kRound)));
+        b[j] = __float_as_uint(y);
     }
-    return __float_as_uint(y);
+    if (far > 0.5f - kNear)
+#pragma unroll
+        for (int j = 0; j < V; ++j) b[j] = exact_quotient(x[j], r.scale);
 }
 __device__ __forceinline__ uint32_t bits_of_size(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
@@ -108,19 +120,14 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __rest
     const RowScale r = row_scale(top);
     int8_t* dst = q + row * ldq;
     const auto put = [&](const Piece<T, V>& p, int c) {
-        if constexpr (V == 1) dst[c] = (int8_t)quantized(to_float(p.v[0]), r);
-        else {
-            uint32_t w[V / 4];
+        float v[V];
+        uint32_t b[V];
 #pragma unroll
-            for (int j = 0; j < V / 4; ++j) {
-                uint32_t b[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) b[k] = quantized(to_float(p.v[4 * j + k]), r);
-                w[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040u), __byte_perm(b[2], b[3], 0x0040u), 0x5410u);
-            }
-            if constexpr (V == 8) *(uint2*)(dst + c) = make_uint2(w[0], w[1]);
-            else *(uint32_t*)(dst + c) = w[0];
-        }
+        for (int j = 0; j < V; ++j) v[j] = to_float(p.v[j]);
+        quantized(b, v, r);
+        if constexpr (V == 1) dst[c] = (int8_t)(b[0] & r.mask);
+        else if constexpr (V == 8) *(uint2*)(dst + c) = make_uint2(low_bytes(b) & r.mask, low_bytes(b + 4) & r.mask);
+        else *(uint32_t*)(dst + c) = low_bytes(b) & r.mask;
     };
     if (KEEP) {
 #pragma unroll
@@ -133,59 +140,78 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __rest
     if (threadIdx.x % (32 * W) == 0) scale[row] = r.scale;
 }
 
-// 32 rows to a block, a row to a lane; warp w reads columns 4 w .. 4 w + 3 of every 32.  KEEP: at most kKeep columns, held in registers.
-constexpr int kSlab = 256, kKeep = kSlab, kSlabPitch = kSlab + 4;    // an odd number of words: the lanes of a store lie in different banks
+// 32 P rows to a block, rows lane, 32 + lane, ... to a lane (256 bytes of a plane are read together); warp w reads columns 4 w .. 4 w + 3 of every 32.
+// KEEP: at most kSlab columns, held in registers.
+constexpr int kSlab = 256, kSlabPitch = kSlab + 4;          // an odd number of words: the lanes of a store lie in different banks
 template <typename T, bool KEEP>
 __global__ void __launch_bounds__(kThreads) quantize_planes_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride,
                                                                    int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale, int words)
 {
-    __shared__ uint32_t tops[8][32];
-    __shared__ __align__(16) uint8_t turned[32 * kSlabPitch];
+    constexpr int P = 8 / sizeof(T), kRows = 32 * P, kMine = kSlab / 8;
+    __shared__ uint32_t tops[8][kRows];
+    __shared__ __align__(16) uint8_t turned[kRows * kSlabPitch];
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
-    const bool mine = row < rows;
-    const T* src = x + (mine ? row : 0) * row_stride;
-    T kept[KEEP ? kKeep / 8 : 4];
-    uint32_t top = 0;
-    if (mine) {
-        if (KEEP) {
+    const int64_t row0 = (int64_t)blockIdx.x * kRows;
+    const T* src[P];
+    bool mine[P];
 #pragma unroll
-            for (int i = 0; i < kKeep / 8; ++i) {
-                const int c = i / 4 * 32 + 4 * warp + i % 4;
-                if (c < cols) kept[i] = src[c * col_stride];
-            }
-#pragma unroll
-            for (int i = 0; i < kKeep / 8; ++i)
-                if (i / 4 * 32 + 4 * warp + i % 4 < cols) top = max(top, bits_of_size(to_float(kept[i])));
-        } else {
-#pragma unroll 8
-            for (int c = warp; c < cols; c += 8) top = max(top, bits_of_size(to_float(src[c * col_stride])));
-        }
+    for (int u = 0; u < P; ++u) {
+        mine[u] = row0 + 32 * u + lane < rows;
+        src[u] = x + (mine[u] ? row0 + 32 * u + lane : 0) * row_stride;
     }
-    tops[warp][lane] = top;
-    __syncthreads();
+    T kept[P][KEEP ? kMine : 1];
+    uint32_t top[P] = {};
+    if (KEEP) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, tops[i][lane]);
-    const RowScale r = row_scale(top);
-    if (warp == 0 && mine) scale[row] = r.scale;
+        for (int i = 0; i < kMine; ++i) {
+            const int c = i / 4 * 32 + 4 * warp + i % 4;
+#pragma unroll
+            for (int u = 0; u < P; ++u)
+                if (c < cols && mine[u]) kept[u][i] = src[u][c * col_stride];
+        }
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+#pragma unroll
+            for (int u = 0; u < P; ++u)
+                if (i / 4 * 32 + 4 * warp + i % 4 < cols && mine[u]) top[u] = max(top[u], bits_of_size(to_float(kept[u][i])));
+    } else {
+#pragma unroll 8
+        for (int c = warp; c < cols; c += 8)
+#pragma unroll
+            for (int u = 0; u < P; ++u)
+                if (mine[u]) top[u] = max(top[u], bits_of_size(to_float(src[u][c * col_stride])));
+    }
+#pragma unroll
+    for (int u = 0; u < P; ++u) tops[warp][32 * u + lane] = top[u];
+    __syncthreads();
+    RowScale r[P];
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[u] = max(top[u], tops[i][32 * u + lane]);
+        r[u] = row_scale(top[u]);
+        if (warp == 0 && mine[u]) scale[row0 + 32 * u + lane] = r[u].scale;
+    }
     for (int slab = 0; slab < cols; slab += kSlab) {
         const int n = min(cols - slab, kSlab);
-        if (mine) {
+#pragma unroll
+        for (int u = 0; u < P; ++u)
 #pragma unroll
             for (int i = 0; i < kSlab / 32; ++i) {
                 const int c = i * 32 + 4 * warp;
-                if (c >= n) continue;
-                uint32_t b[4] = {};
+                if (c >= n || !mine[u]) continue;
+                float v[4] = {};
+                uint32_t b[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (c + k < n) b[k] = quantized(to_float(KEEP ? kept[KEEP ? 4 * i + k : 0] : src[(slab + c + k) * col_stride]), r);
-                *(uint32_t*)(turned + lane * kSlabPitch + c) = __byte_perm(__byte_perm(b[0], b[1], 0x0040u), __byte_perm(b[2], b[3], 0x0040u), 0x5410u);
+                    if (c + k < n) v[k] = to_float(KEEP ? kept[u][KEEP ? 4 * i + k : 0] : src[u][(slab + c + k) * col_stride]);
+                quantized(b, v, r[u]);
+                *(uint32_t*)(turned + (32 * u + lane) * kSlabPitch + c) = low_bytes(b) & r[u].mask;
             }
-        }
         __syncthreads();
-        for (int i = warp; i < 32 && row0 + i < rows; i += 8) {
+        for (int i = warp; i < kRows && row0 + i < rows; i += 8) {
             int8_t* dst = q + (row0 + i) * ldq + slab;
             const uint8_t* from = turned + i * kSlabPitch;
             const int whole = words ? n / 4 : 0;
@@ -205,8 +231,9 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
     const int n = (int)cols;
     if (cs != 1 && cols > 1) {
         const int words = aligned(q, 4) && (ldq % 4 == 0 || rows == 1);
-        const dim3 grid((unsigned)((rows + 31) / 32));
-        return n <= kKeep ? launch_early(early, quantize_planes_kernel<T, true>, grid, dim3(kThreads), 0, s, x, rows, n, rs, cs, q, ldq, scale, words)
+        constexpr int per = 32 * 8 / sizeof(T);
+        const dim3 grid((unsigned)((rows + per - 1) / per));
+        return n <= kSlab ? launch_early(early, quantize_planes_kernel<T, true>, grid, dim3(kThreads), 0, s, x, rows, n, rs, cs, q, ldq, scale, words)
                           : launch_early(early, quantize_planes_kernel<T, false>, grid, dim3(kThreads), 0, s, x, rows, n, rs, cs, q, ldq, scale, words);
     }
     constexpr int V = 16 / sizeof(T);
