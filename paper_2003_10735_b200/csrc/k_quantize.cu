@@ -2,13 +2,13 @@
 // the nearest whole number (half to even), exactly.
 //
 // Bound by memory: 4 or 2 bytes read and 1 written per value.  Two forms, both reading x once where a row fits registers:
-//   rows whose values lie side by side (tokens, weights): 1 to 8 warps to a row
-//   other strides (planar feature maps, whose rows are pixels): a block takes 32 rows and reads them channel by channel, a row to a
-//     lane, so that planes are read in whole sectors; the integers are turned round in shared memory
+//   rows whose values lie side by side (tokens, weights): 1 to 8 warps to a row, 16 bytes to an access wherever a row begins
+//   other strides (planar feature maps, whose rows are pixels): a block takes 64 or 128 rows and reads them channel by channel, so that
+//     planes are read 256 bytes at a time; the integers are turned round in shared memory
 //
 // The quotient is x * (1 / scale), off by at most 127 * 2^-23 of a step (1.5e-5), so it gives the whole number unless it lies within kNear
-// of a half.  There (one value in 25000; a lane then takes all values of its piece that way) the quotient in double decides: of two fp32
-// numbers it is either a half exactly or at least 2^-32 away from one.
+// of a half h.  There the sign of x - h scale decides, which a fused multiply-add has exactly.  Rows whose scale is so small that this could
+// underflow take the quotient in double: of two fp32 numbers it is either a half exactly or at least 2^-32 away from one.
 #include "../../include/shadowtutor.h"
 #include "st_internal.h"
 #include "int8_common.h"
@@ -29,8 +29,70 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 
-// `doubt`: added to a value's distance from the whole numbers; 1 sends every value through the quotient in double.  `mask`: 0 makes all integers 0.
-struct RowScale { float scale, inverse, doubt; uint32_t mask; };
+// 16 bytes of a row, and the largest |x| met so far (NaN if one was NaN); 16-bit types in pairs
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+    static constexpr int V = 4;
+    float v[4];
+    __device__ __forceinline__ void get(float (&x)[4]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = v[j];
+    }
+};
+template <> struct Piece<bf16> {
+    static constexpr int V = 8;
+    __nv_bfloat162 v[4];
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = __low2float(v[j]); x[2 * j + 1] = __high2float(v[j]); }
+    }
+};
+template <> struct Piece<__half> {
+    static constexpr int V = 8;
+    __half2 v[4];
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = __low2float(v[j]); x[2 * j + 1] = __high2float(v[j]); }
+    }
+};
+__device__ __forceinline__ float larger(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+template <typename T> struct Top;
+template <> struct Top<float> {
+    float t = 0.f;
+    __device__ __forceinline__ void add(const Piece<float>& p)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t = larger(t, fabsf(p.v[j]));
+    }
+    __device__ __forceinline__ void add(float x) { t = larger(t, fabsf(x)); }
+    __device__ __forceinline__ uint32_t bits() const { return __float_as_uint(t) & 0x7fffffffu; }
+};
+template <> struct Top<bf16> {
+    __nv_bfloat162 t = {0, 0};
+    __device__ __forceinline__ void add(const Piece<bf16>& p)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t = __hmax2_nan(t, __habs2(p.v[j]));
+    }
+    __device__ __forceinline__ void add(bf16 x) { t.x = __hmax_nan(t.x, __habs(x)); }
+    __device__ __forceinline__ uint32_t bits() const { return __float_as_uint(larger(__low2float(t), __high2float(t))) & 0x7fffffffu; }
+};
+template <> struct Top<__half> {
+    __half2 t = {0, 0};
+    __device__ __forceinline__ void add(const Piece<__half>& p)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t = __hmax2_nan(t, __habs2(p.v[j]));
+    }
+    __device__ __forceinline__ void add(__half x) { t.x = __hmax_nan(t.x, __habs(x)); }
+    __device__ __forceinline__ uint32_t bits() const { return __float_as_uint(larger(__low2float(t), __high2float(t))) & 0x7fffffffu; }
+};
+
+// `doubt`: 0, or 1 for a row whose values take the quotient in double.  `mask`: 0 makes all integers 0.
+struct __align__(16) RowScale { float scale, inverse, doubt; uint32_t mask; };
 // From the bits of the row's largest |x| (NaN lies above infinity).  A row that is not finite has scale NaN and integers 0.
 __device__ __forceinline__ RowScale row_scale(uint32_t top)
 {
@@ -42,183 +104,276 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top)
     r.mask = finite ? 0xffffffffu : 0u;
     return r;
 }
-__device__ __noinline__ uint32_t exact_quotient(float x, float scale)
-{
-    const double q = rint((double)x / (double)scale);
-    return (uint32_t)(int)fmin(fmax(q, -127.0), 127.0);
-}
 __device__ __forceinline__ uint32_t low_bytes(const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0040u), __byte_perm(c[2], c[3], 0x0040u), 0x5410u); }
-// the integers of V values in the low bytes of words
-template <int V>
-__device__ __forceinline__ void quantized(uint32_t (&b)[V], const float (&x)[V], const RowScale& r)
+// The integers of n <= 4 values, read again, from quotients in double; packed
+template <typename T>
+__device__ __noinline__ uint32_t exact_integers(const T* x, int64_t stride, int n, float scale)
+{
+    uint32_t w = 0;
+    for (int j = 0; j < n; ++j) {
+        const double q = rint((double)to_float(x[j * stride]) / (double)scale);
+        w |= ((uint32_t)(int)fmin(fmax(q, -127.0), 127.0) & 0xffu) << (8 * j);
+    }
+    return w;
+}
+// x / scale to the nearest whole number, for a quotient t next to a half
+__device__ __forceinline__ float beside_half(float x, float t, float scale)
+{
+    const float k = (t + kRound) - kRound, d = t - k;
+    if (fabsf(d) <= 0.5f - kNear) return k;
+    const float h = k + copysignf(0.5f, d), over = fmaf(-h, scale, x);
+    return over > 0.f ? h + 0.5f : over < 0.f ? h - 0.5f : rintf(h);
+}
+// The integers of V values (4 or 8) that lie at `at`, packed in words
+template <typename T, int V>
+__device__ __forceinline__ void quantize(uint32_t (&w)[V / 4], const float (&x)[V], const T* at, int64_t stride, int n, const RowScale& r)
 {
     float far = r.doubt;
+    uint32_t b[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float t = x[j] * r.inverse, y = t + kRound;
-        far = fmaxf(far, fabsf(t - (y - kRound)));
-        b[j] = __float_as_uint(y);
+    for (int j = 0; j < V; j += 2) {
+        unsigned long long t, y, d;             // two values to an instruction
+        asm("{\n\t.reg .b64 v, s, up, down, minus;\n\t"
+            "mov.b64 v, {%3, %4};\n\tmov.b64 s, {%5, %5};\n\tmov.b64 up, {%6, %6};\n\tmov.b64 down, {%7, %7};\n\tmov.b64 minus, {%8, %8};\n\t"
+            "mul.rn.f32x2 %0, v, s;\n\tadd.rn.f32x2 %1, %0, up;\n\tadd.rn.f32x2 %2, %1, down;\n\tfma.rn.f32x2 %2, %2, minus, %0;\n\t}"
+            : "=&l"(t), "=&l"(y), "=&l"(d) : "f"(x[j]), "f"(x[j + 1]), "f"(r.inverse), "f"(kRound), "f"(-kRound), "f"(-1.f));
+        far = fmaxf(far, fmaxf(fabsf(__uint_as_float((uint32_t)d)), fabsf(__uint_as_float((uint32_t)(d >> 32)))));
+        b[j] = (uint32_t)y;
+        b[j + 1] = (uint32_t)(y >> 32);
     }
-    if (far > 0.5f - kNear)
+    if (far > 0.5f - kNear && r.doubt == 0.f)
 #pragma unroll
-        for (int j = 0; j < V; ++j) b[j] = exact_quotient(x[j], r.scale);
+        for (int j = 0; j < V; ++j) b[j] = __float_as_uint(beside_half(x[j], x[j] * r.inverse, r.scale) + kRound);
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = low_bytes(b + 4 * i) & r.mask;
+    if (r.doubt != 0.f)
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) w[i] = exact_integers(at + 4 * i * stride, stride, min(n - 4 * i, 4), r.scale);
 }
-__device__ __forceinline__ uint32_t bits_of_size(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-template <typename T, int V> struct Piece { T v[V]; };
-template <typename T, int V>
-__device__ __forceinline__ void load_piece(Piece<T, V>& p, const T* src)
+template <typename T>
+__device__ __forceinline__ uint8_t quantize_one(const T* at, const RowScale& r)
 {
-    if constexpr (V == 1) p.v[0] = *src;
-    else *(uint4*)p.v = *(const uint4*)src;
+    const float x = to_float(*at);
+    if (r.doubt != 0.f) return (uint8_t)exact_integers(at, 0, 1, r.scale);
+    return (uint8_t)(__float_as_uint(beside_half(x, x * r.inverse, r.scale) + kRound) & r.mask);
 }
 
-// W warps to a row, V values to an access (16 bytes, or one value).  KEEP: the row fits ITEMS pieces per lane; otherwise it is read twice.
-template <typename T, int V, int W, bool KEEP>
+// A row's memory: `head` single values up to a 16-byte boundary, `pieces` of 16 bytes, single values from `tail` on.
+struct RowParts { int head, pieces, tail; };
+template <typename T>
+__device__ __forceinline__ RowParts parts_of(const T* row, int cols)
+{
+    constexpr int V = Piece<T>::V;
+    RowParts p;
+    p.head = min((int)((16u - ((uint32_t)(uintptr_t)row & 15u)) & 15u) / (int)sizeof(T), cols);
+    p.pieces = (cols - p.head) / V;
+    p.tail = p.head + p.pieces * V;
+    return p;
+}
+
+// W warps to a row.  ALIGNED: rows of x and q begin where whole pieces can be read and written, and cols is a multiple of V.  Otherwise the integers
+// of a row are gathered in shared memory and written from there in aligned words, whatever the alignment of x's and q's rows.
+// KEEP: a row fits kItems pieces per lane; otherwise it is read twice, the second time in stretches of that many.
+constexpr int kItems = 8;
+template <typename T, int W, bool ALIGNED, bool KEEP>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride,
                                                                  int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale)
 {
-    constexpr int ITEMS = V == 1 ? 16 : 4, STEP = 32 * W * V, kRows = kThreads / 32 / W;
+    constexpr int V = Piece<T>::V, kLanes = 32 * W, kRows = kThreads / kLanes, kStretch = kItems * kLanes;     // pieces
+    constexpr int kPitch = kStretch * V + 32;               // bytes of a row's stretch with its head and tail, and what aligning it takes
     __shared__ uint32_t tops[kThreads / 32];
+    __shared__ __align__(16) uint8_t gathered[ALIGNED ? 16 : kRows * kPitch];
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, at = (threadIdx.x % (32 * W)) * V;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, me = threadIdx.x % kLanes;
     const int64_t row = (int64_t)blockIdx.x * kRows + warp / W;
-    if (W == 1 && row >= rows) return;
     const bool mine = row < rows;
-    const T* src = x + row * row_stride;
-    Piece<T, V> kept[KEEP ? ITEMS : 1];
-    uint32_t top = 0;
+    if (W == 1 && !mine) return;
+    const T* src = x + (mine ? row : 0) * row_stride;
+    int8_t* dst = q + (mine ? row : 0) * ldq;
+    const RowParts p = ALIGNED ? RowParts{0, cols / V, cols} : parts_of(src, cols);
+    const uint4* body = (const uint4*)(src + p.head);
+    Piece<T> kept[kItems];
+    Top<T> top;
+    const auto get = [&](Piece<T>& k, int i) { *(uint4*)k.v = body[i]; };
     if (mine) {
         if (KEEP) {
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i)
-                if (at + i * STEP < cols) load_piece(kept[i], src + at + i * STEP);
+            for (int i = 0; i < kItems; ++i)
+                if (me + i * kLanes < p.pieces) get(kept[i], me + i * kLanes);
+        }
+        if (!ALIGNED) {
+            if (me < p.head) top.add(src[me]);
+            if (p.tail + me < cols) top.add(src[p.tail + me]);
+        }
+        if (KEEP) {
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i)
-                if (at + i * STEP < cols) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) top = max(top, bits_of_size(to_float(kept[i].v[j])));
-                }
+            for (int i = 0; i < kItems; ++i)
+                if (me + i * kLanes < p.pieces) top.add(kept[i]);
         } else {
 #pragma unroll 4
-            for (int c = at; c < cols; c += STEP) {
-                load_piece(kept[0], src + c);
-#pragma unroll
-                for (int j = 0; j < V; ++j) top = max(top, bits_of_size(to_float(kept[0].v[j])));
-            }
+            for (int i = me; i < p.pieces; i += kLanes) { get(kept[0], i); top.add(kept[0]); }
         }
     }
-    top = __reduce_max_sync(0xffffffffu, top);
+    uint32_t bits = __reduce_max_sync(0xffffffffu, top.bits());
     if (W > 1) {
-        if (lane == 0) tops[warp] = top;
+        if (lane == 0) tops[warp] = bits;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < W; ++i) top = max(top, tops[warp / W * W + i]);
-        if (!mine) return;
+        for (int i = 0; i < W; ++i) bits = max(bits, tops[warp / W * W + i]);
     }
-    const RowScale r = row_scale(top);
-    int8_t* dst = q + row * ldq;
-    const auto put = [&](const Piece<T, V>& p, int c) {
+    const RowScale r = row_scale(bits);
+    if (mine && me == 0) scale[row] = r.scale;
+    const auto pack = [&](uint32_t (&w)[V / 4], const Piece<T>& k, int i) {
         float v[V];
-        uint32_t b[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = to_float(p.v[j]);
-        quantized(b, v, r);
-        if constexpr (V == 1) dst[c] = (int8_t)(b[0] & r.mask);
-        else if constexpr (V == 8) *(uint2*)(dst + c) = make_uint2(low_bytes(b) & r.mask, low_bytes(b + 4) & r.mask);
-        else *(uint32_t*)(dst + c) = low_bytes(b) & r.mask;
+        k.get(v);
+        quantize<T, V>(w, v, src + p.head + i * V, 1, V, r);
     };
-    if (KEEP) {
+    if (ALIGNED) {
+        if (!mine) return;
+        const auto put = [&](const Piece<T>& k, int i) {
+            uint32_t w[V / 4];
+            pack(w, k, i);
+            if constexpr (V == 8) *(uint2*)(dst + i * V) = make_uint2(w[0], w[1]);
+            else *(uint32_t*)(dst + i * V) = w[0];
+        };
+        if (KEEP) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-            if (at + i * STEP < cols) put(kept[i], at + i * STEP);
-    } else {
+            for (int i = 0; i < kItems; ++i)
+                if (me + i * kLanes < p.pieces) put(kept[i], me + i * kLanes);
+        } else {
 #pragma unroll 4
-        for (int c = at; c < cols; c += STEP) { load_piece(kept[0], src + c); put(kept[0], c); }
+            for (int i = me; i < p.pieces; i += kLanes) { get(kept[0], i); put(kept[0], i); }
+        }
+        return;
     }
-    if (threadIdx.x % (32 * W) == 0) scale[row] = r.scale;
+    // integer c of the row lies at buf[c - first]; buf is placed so that pieces lie at multiples of 8
+    uint8_t* const area = gathered + (threadIdx.x / kLanes) * kPitch;
+    for (int begin = 0; begin == 0 || begin < p.pieces; begin += kStretch) {
+        const bool is_first = begin == 0, is_last = begin + kStretch >= p.pieces;
+        const int first = is_first ? 0 : p.head + begin * V, last = is_last ? cols : p.head + (begin + kStretch) * V;
+        uint8_t* const buf = area + ((8 - p.head) & 7) * is_first;
+        if (mine) {
+            if (is_first && me < p.head) buf[me] = quantize_one(src + me, r);
+            if (is_last && p.tail + me < cols) buf[p.tail + me - first] = quantize_one(src + p.tail + me, r);
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                const int at = begin + me + i * kLanes;
+                if (at >= p.pieces) continue;
+                if (!KEEP) get(kept[i], at);
+                uint32_t w[V / 4];
+                pack(w, kept[i], at);
+                uint8_t* to = buf + p.head + at * V - first;
+                if constexpr (V == 8) *(uint2*)to = make_uint2(w[0], w[1]);
+                else *(uint32_t*)to = w[0];
+            }
+        }
+        if (W == 1) __syncwarp(); else __syncthreads();
+        if (mine) {
+            // single bytes up to the first word of q, words put together from two of the buffer's, single bytes behind
+            const int n = last - first, lead = min((int)(-(uint32_t)(uintptr_t)(dst + first) & 3u), n), words = (n - lead) / 4;
+            if (me < lead) dst[first + me] = (int8_t)buf[me];
+            const uint32_t off = (uint32_t)(uintptr_t)(buf + lead) & 3u;
+            const uint32_t* from = (const uint32_t*)(buf + lead - off);
+            uint32_t* to = (uint32_t*)(dst + first + lead);
+            for (int i = me; i < words; i += kLanes) to[i] = off ? __funnelshift_r(from[i], from[i + 1], 8 * off) : from[i];
+            if (lead + 4 * words + me < n) dst[first + lead + 4 * words + me] = (int8_t)buf[lead + 4 * words + me];
+        }
+        if (W == 1) __syncwarp(); else __syncthreads();
+    }
 }
 
-// 32 P rows to a block, rows lane, 32 + lane, ... to a lane (256 bytes of a plane are read together); warp w reads columns 4 w .. 4 w + 3 of every 32.
-// KEEP: at most kSlab columns, held in registers.
-constexpr int kSlab = 256, kSlabPitch = kSlab + 4;          // an odd number of words: the lanes of a store lie in different banks
-template <typename T, bool KEEP>
-__global__ void __launch_bounds__(kThreads) quantize_planes_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride,
-                                                                   int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale, int words)
+// Rows whose values do not lie side by side.  A block takes 32 P rows, rows lane, 32 + lane, ... to a lane (256 bytes of a plane are read together);
+// warp w reads columns 4 w .. 4 w + 3 of every 4 kPlaneWarps.  KEEP: at most kSlab columns, held in registers.  Lanes and columns beyond the
+// matrix read its last row and column again, which changes nothing, and write nothing.
+constexpr int kPlaneWarps = 16, kSlab = 256, kSlabPitch = kSlab + 4;        // an odd number of words: the lanes of a store lie in different banks
+template <typename T, bool KEEP, bool UNIT>
+__global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride,
+                                                                              int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale, int words)
 {
-    constexpr int P = 8 / sizeof(T), kRows = 32 * P, kMine = kSlab / 8;
-    __shared__ uint32_t tops[8][kRows];
+    constexpr int P = 8 / sizeof(T), kRows = 32 * P, kGroups = kSlab / 4 / kPlaneWarps;
+    __shared__ uint32_t tops[kPlaneWarps][kRows];
+    __shared__ RowScale scales[kRows];
     __shared__ __align__(16) uint8_t turned[kRows * kSlabPitch];
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t row0 = (int64_t)blockIdx.x * kRows;
-    const T* src[P];
-    bool mine[P];
+    // UNIT: rows lie side by side and all of the block's exist
+    const T* src[UNIT ? 1 : P];
 #pragma unroll
-    for (int u = 0; u < P; ++u) {
-        mine[u] = row0 + 32 * u + lane < rows;
-        src[u] = x + (mine[u] ? row0 + 32 * u + lane : 0) * row_stride;
-    }
-    T kept[P][KEEP ? kMine : 1];
-    uint32_t top[P] = {};
-    if (KEEP) {
+    for (int u = 0; u < (UNIT ? 1 : P); ++u) src[u] = UNIT ? x + row0 + lane : x + min(row0 + 32 * u + lane, rows - 1) * row_stride;
+    T kept[kGroups][4][P];
+    Top<T> top[P];
+    const auto fetch = [&](T (&k)[4][P], int c) {
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int c = i / 4 * 32 + 4 * warp + i % 4;
+        for (int j = 0; j < 4; ++j) {
+            const int64_t at = min(c + j, cols - 1) * col_stride;
 #pragma unroll
-            for (int u = 0; u < P; ++u)
-                if (c < cols && mine[u]) kept[u][i] = src[u][c * col_stride];
+            for (int u = 0; u < P; ++u) k[j][u] = UNIT ? src[0][at + 32 * u] : src[UNIT ? 0 : u][at];
         }
+    };
+    for (int slab = 0; slab < cols; slab += kSlab) {
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
+        for (int i = 0; i < kGroups; ++i)
+            if (slab + 4 * (warp + kPlaneWarps * i) < cols) fetch(kept[i], slab + 4 * (warp + kPlaneWarps * i));
 #pragma unroll
-            for (int u = 0; u < P; ++u)
-                if (i / 4 * 32 + 4 * warp + i % 4 < cols && mine[u]) top[u] = max(top[u], bits_of_size(to_float(kept[u][i])));
-    } else {
-#pragma unroll 8
-        for (int c = warp; c < cols; c += 8)
+        for (int i = 0; i < kGroups; ++i)
+            if (slab + 4 * (warp + kPlaneWarps * i) < cols)
 #pragma unroll
-            for (int u = 0; u < P; ++u)
-                if (mine[u]) top[u] = max(top[u], bits_of_size(to_float(src[u][c * col_stride])));
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int u = 0; u < P; ++u) top[u].add(kept[i][j][u]);
+        if (KEEP) break;
     }
 #pragma unroll
-    for (int u = 0; u < P; ++u) tops[warp][32 * u + lane] = top[u];
+    for (int u = 0; u < P; ++u) tops[warp][32 * u + lane] = top[u].bits();
     __syncthreads();
-    RowScale r[P];
+    if (threadIdx.x < kRows) {
+        uint32_t bits = 0;
 #pragma unroll
-    for (int u = 0; u < P; ++u) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top[u] = max(top[u], tops[i][32 * u + lane]);
-        r[u] = row_scale(top[u]);
-        if (warp == 0 && mine[u]) scale[row0 + 32 * u + lane] = r[u].scale;
+        for (int i = 0; i < kPlaneWarps; ++i) bits = max(bits, tops[i][threadIdx.x]);
+        const RowScale r = row_scale(bits);
+        scales[threadIdx.x] = r;
+        if (row0 + threadIdx.x < rows) scale[row0 + threadIdx.x] = r.scale;
     }
+    __syncthreads();
     for (int slab = 0; slab < cols; slab += kSlab) {
         const int n = min(cols - slab, kSlab);
+        if (!KEEP) {
 #pragma unroll
-        for (int u = 0; u < P; ++u)
+            for (int i = 0; i < kGroups; ++i)
+                if (4 * (warp + kPlaneWarps * i) < n) fetch(kept[i], slab + 4 * (warp + kPlaneWarps * i));
+        }
 #pragma unroll
-            for (int i = 0; i < kSlab / 32; ++i) {
-                const int c = i * 32 + 4 * warp;
-                if (c >= n || !mine[u]) continue;
-                float v[4] = {};
-                uint32_t b[4];
+        for (int u = 0; u < P; ++u) {
+            const RowScale r = scales[32 * u + lane];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < n) v[k] = to_float(KEEP ? kept[u][KEEP ? 4 * i + k : 0] : src[u][(slab + c + k) * col_stride]);
-                quantized(b, v, r[u]);
-                *(uint32_t*)(turned + (32 * u + lane) * kSlabPitch + c) = low_bytes(b) & r[u].mask;
+            for (int i = 0; i < kGroups; ++i) {
+                const int c = 4 * (warp + kPlaneWarps * i);
+                if (c >= n) continue;
+                const float v[4] = {to_float(kept[i][0][u]), to_float(kept[i][1][u]), to_float(kept[i][2][u]), to_float(kept[i][3][u])};
+                uint32_t w[1];
+                quantize<T, 4>(w, v, (UNIT ? src[0] + 32 * u : src[UNIT ? 0 : u]) + (slab + c) * col_stride, col_stride, n - c, r);
+                *(uint32_t*)(turned + (32 * u + lane) * kSlabPitch + c) = w[0];
             }
-        __syncthreads();
-        for (int i = warp; i < kRows && row0 + i < rows; i += 8) {
-            int8_t* dst = q + (row0 + i) * ldq + slab;
-            const uint8_t* from = turned + i * kSlabPitch;
-            const int whole = words ? n / 4 : 0;
-            for (int c = lane; c < whole; c += 32) ((uint32_t*)dst)[c] = *(const uint32_t*)(from + 4 * c);
-            for (int c = 4 * whole + lane; c < n; c += 32) dst[c] = (int8_t)from[c];
         }
         __syncthreads();
+        const int rows_in = (int)min((int64_t)kRows, rows - row0);
+        for (int i = warp; i < rows_in; i += kPlaneWarps) {
+            int8_t* dst = q + (row0 + i) * ldq + slab;
+            const uint8_t* from = turned + i * kSlabPitch;
+            if (words && n == kSlab) {
+                const uint32_t a = *(const uint32_t*)(from + 4 * lane), b = *(const uint32_t*)(from + 128 + 4 * lane);
+                ((uint32_t*)dst)[lane] = a;
+                ((uint32_t*)dst)[32 + lane] = b;
+            } else {
+                const int whole = words ? n / 4 : 0;
+                for (int c = lane; c < whole; c += 32) ((uint32_t*)dst)[c] = *(const uint32_t*)(from + 4 * c);
+                for (int c = 4 * whole + lane; c < n; c += 32) dst[c] = (int8_t)from[c];
+            }
+        }
+        if (!KEEP) __syncthreads();
     }
 }
 
@@ -232,30 +387,37 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
     if (cs != 1 && cols > 1) {
         const int words = aligned(q, 4) && (ldq % 4 == 0 || rows == 1);
         constexpr int per = 32 * 8 / sizeof(T);
-        const dim3 grid((unsigned)((rows + per - 1) / per));
-        return n <= kSlab ? launch_early(early, quantize_planes_kernel<T, true>, grid, dim3(kThreads), 0, s, x, rows, n, rs, cs, q, ldq, scale, words)
-                          : launch_early(early, quantize_planes_kernel<T, false>, grid, dim3(kThreads), 0, s, x, rows, n, rs, cs, q, ldq, scale, words);
+        const auto go = [&](auto kernel, const T* from, int64_t first, int64_t count) {
+            return launch_early(early, kernel, dim3((unsigned)((count + per - 1) / per)), dim3(32 * kPlaneWarps), 0, s, from, count, n, rs, cs, q + first * ldq, ldq, scale + first, words);
+        };
+        // whole blocks of pixels that lie side by side, then what is left
+        const int64_t unit = rs == 1 ? rows / per * per : 0;
+        cudaError_t e = cudaSuccess;
+        if (unit) e = n <= kSlab ? go(quantize_planes_kernel<T, true, true>, x, 0, unit) : go(quantize_planes_kernel<T, false, true>, x, 0, unit);
+        if (e == cudaSuccess && unit < rows)
+            e = n <= kSlab ? go(quantize_planes_kernel<T, true, false>, x + unit * rs, unit, rows - unit) : go(quantize_planes_kernel<T, false, false>, x + unit * rs, unit, rows - unit);
+        return e;
     }
-    constexpr int V = 16 / sizeof(T);
-    const bool vec = aligned(x, 16) && (rows == 1 || rs * sizeof(T) % 16 == 0) && cols % V == 0 && aligned(q, V) && (rows == 1 || ldq % V == 0);
+    constexpr int V = Piece<T>::V;
+    const bool whole = aligned(x, 16) && (rows == 1 || rs * sizeof(T) % 16 == 0) && cols % V == 0 && aligned(q, V) && (rows == 1 || ldq % V == 0);
     const auto go = [&](auto kernel, int warps) {
         const int per = kThreads / 32 / warps;
         return launch_early(early, kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kThreads), 0, s, x, rows, n, rs, q, ldq, scale);
     };
-    // as few warps to a row as hold it in registers: 32 values per lane in pieces of 16 bytes, 16 single ones
-    const int64_t room = vec ? 32 * 4 * V : 32 * 16;
-    if (vec) {
-        if (cols <= room) return go(quantize_rows_kernel<T, V, 1, true>, 1);
-        if (cols <= 2 * room) return go(quantize_rows_kernel<T, V, 2, true>, 2);
-        if (cols <= 4 * room) return go(quantize_rows_kernel<T, V, 4, true>, 4);
-        if (cols <= 8 * room) return go(quantize_rows_kernel<T, V, 8, true>, 8);
-        return go(quantize_rows_kernel<T, V, 8, false>, 8);
+    // as few warps to a row as hold it in registers
+    const int64_t room = 32 * kItems * V;
+    if (whole) {
+        if (cols <= room) return go(quantize_rows_kernel<T, 1, true, true>, 1);
+        if (cols <= 2 * room) return go(quantize_rows_kernel<T, 2, true, true>, 2);
+        if (cols <= 4 * room) return go(quantize_rows_kernel<T, 4, true, true>, 4);
+        if (cols <= 8 * room) return go(quantize_rows_kernel<T, 8, true, true>, 8);
+        return go(quantize_rows_kernel<T, 8, true, false>, 8);
     }
-    if (cols <= room) return go(quantize_rows_kernel<T, 1, 1, true>, 1);
-    if (cols <= 2 * room) return go(quantize_rows_kernel<T, 1, 2, true>, 2);
-    if (cols <= 4 * room) return go(quantize_rows_kernel<T, 1, 4, true>, 4);
-    if (cols <= 8 * room) return go(quantize_rows_kernel<T, 1, 8, true>, 8);
-    return go(quantize_rows_kernel<T, 1, 8, false>, 8);
+    if (cols <= room) return go(quantize_rows_kernel<T, 1, false, true>, 1);
+    if (cols <= 2 * room) return go(quantize_rows_kernel<T, 2, false, true>, 2);
+    if (cols <= 4 * room) return go(quantize_rows_kernel<T, 4, false, true>, 4);
+    if (cols <= 8 * room) return go(quantize_rows_kernel<T, 8, false, true>, 8);
+    return go(quantize_rows_kernel<T, 8, false, false>, 8);
 }
 
 }  // namespace
