@@ -45,6 +45,10 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"((uint64_t)map), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 struct Out {
@@ -77,17 +81,18 @@ __device__ __forceinline__ void put_one(const Out& o, int64_t at, float y)
 // ---- many tokens ------------------------------------------------------------------------------------------------
 constexpr int kTilesThreads = 384;              // producer, issuer, two idle warps (registers), eight that store
 // `stall`: 0; a test of the give-up path makes the first stage expect bytes that no copy delivers, so that the waits behind it run out
+constexpr int kPieceRow = 64, kPieceBytes = 32 * kPieceRow;        // what a warp stages at a time: 32 rows of 64 bytes
 struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices; unsigned int* err; uint32_t stall; };
 
 template <int BN>
 struct TilesShape {
     static constexpr int stage_bytes = (kTile + BN) * kSlice, stages = (int)(192 * 1024 / stage_bytes) < 8 ? (int)(192 * 1024 / stage_bytes) : 8;
-    static constexpr size_t bytes = (size_t)stages * stage_bytes + kSmemAlign;
+    static constexpr size_t bytes = (size_t)stages * stage_bytes + 8 * kPieceBytes + kSmemAlign;
     static constexpr int acc_cols = BN < 32 ? 32 : BN;
 };
 
 template <int BN>
-__global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const TilesArgs a)
+__global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
 {
     using Shape = TilesShape<BN>;
     constexpr int S = Shape::stages;
@@ -95,8 +100,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     const uint32_t ring = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1);
     __shared__ __align__(8) uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
-    __shared__ float turned[8][32 * 17];
-    __shared__ float column[2][2][BN];          // per accumulator: scales and bias of its columns
+    __shared__ __align__(16) float column[2][2][BN];         // per accumulator: scales and bias of its columns
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), 2 * Shape::acc_cols);
     if (threadIdx.x == 0) {
@@ -159,6 +163,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
         const int half = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * half;
         const Out& o = a.out;
         uint32_t acc = 0, acc_phase = 0;
+        const uint32_t piece = ring + S * Shape::stage_bytes + (warp - 4) * kPieceBytes;
         for (int t = (int)blockIdx.x; t < tiles; t += gridDim.x) {
             const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
             const int64_t row = (int64_t)m0 + quarter * 32 + lane;
@@ -173,40 +178,60 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
             // a warp whose wait has given up goes on through the tiles without storing: the others wait for it above
             if (ok) ok = mbar_wait(smem_u32(&acc_full[acc]), acc_phase, a.err, kWaitDone);
             tc_fence_after_sync();
+            const int rows_in = min(min(a.tile_m, o.M - m0) - quarter * 32, 32);       // of this warp's 32
+            // TMA leaves out the rows and the 16-byte pieces that lie beyond y, but not the rest of a piece that y ends in
+            const bool whole_end = o.N * (o.type == ST_F32 ? 4 : 2) % 16 == 0;
+            const CUtensorMap* tm_out = a.tile_m - quarter * 32 >= 32 ? &tm_y : &tm_y_rest;
 #pragma unroll 1
-            for (int c0 = half * (BN / 2); ok && c0 < (half + 1) * (BN / 2) && n0 + c0 < o.N; c0 += 32) {
+            for (int c0 = half * (BN / 2); ok && c0 < (half + 1) * (BN / 2) && n0 + c0 < o.N && rows_in > 0; c0 += 32) {
                 float v[32];
                 __syncwarp();
                 tmem_ld_32x32(tmem + acc * Shape::acc_cols + ((uint32_t)(quarter * 32) << 16) + c0, v);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = finish(__float_as_int(v[j]), sx, column[acc][0][c0 + j], column[acc][1][c0 + j], o.bias != nullptr, o.relu);
-                const int64_t at = row * o.ldy + n0 + c0;
-                if (o.wide && n0 + c0 + 32 <= o.N) {
-                    if (!mine) continue;
-                    if (o.type == ST_F32) {
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 sw = *(const float4*)&column[acc][0][c0 + j], b = *(const float4*)&column[acc][1][c0 + j];
+                    v[j] = finish(__float_as_int(v[j]), sx, sw.x, b.x, o.bias != nullptr, o.relu);
+                    v[j + 1] = finish(__float_as_int(v[j + 1]), sx, sw.y, b.y, o.bias != nullptr, o.relu);
+                    v[j + 2] = finish(__float_as_int(v[j + 2]), sx, sw.z, b.z, o.bias != nullptr, o.relu);
+                    v[j + 3] = finish(__float_as_int(v[j + 3]), sx, sw.w, b.w, o.bias != nullptr, o.relu);
+                }
+                if (o.wide && (whole_end || n0 + c0 + 32 <= o.N)) {
+                    // rows of 64 bytes, 16-byte pieces where TMA's 64-byte swizzle has them (no two lanes of a store in one bank), one copy
+                    const int passes = o.type == ST_F32 ? 2 : 1;
+                    for (int h = 0; h < passes; ++h) {
+                        if (lane == 0) tma_store_wait_read<0>();
+                        __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) *(float4*)((float*)o.y + at + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            *(uint4*)((uint16_t*)o.y + at + j) = make_uint4(round16x2(v[j], v[j + 1], o.type), round16x2(v[j + 2], v[j + 3], o.type),
-                                                                           round16x2(v[j + 4], v[j + 5], o.type), round16x2(v[j + 6], v[j + 7], o.type));
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t to = piece + lane * kPieceRow + ((k ^ ((lane >> 1) & 3)) * 16);
+                            if (o.type == ST_F32) {
+                                const float *lo = v + 4 * k, *hi = v + 16 + 4 * k;
+                                st_shared_128(to, __float_as_uint(h ? hi[0] : lo[0]), __float_as_uint(h ? hi[1] : lo[1]), __float_as_uint(h ? hi[2] : lo[2]), __float_as_uint(h ? hi[3] : lo[3]));
+                            } else {
+                                st_shared_128(to, round16x2(v[8 * k], v[8 * k + 1], o.type), round16x2(v[8 * k + 2], v[8 * k + 3], o.type),
+                                              round16x2(v[8 * k + 4], v[8 * k + 5], o.type), round16x2(v[8 * k + 6], v[8 * k + 7], o.type));
+                            }
+                        }
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0 && n0 + c0 + 16 * h < o.N) { tma_store_2d(tm_out, piece, n0 + c0 + 16 * h, m0 + quarter * 32); tma_store_commit(); }
                     }
                 } else {
                     // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
-                    // 157 us with each lane storing its own row value by value)
-                    float* piece = turned[warp - 4];
-                    const int rows_in = min(min(a.tile_m, o.M - m0) - quarter * 32, 32), r0 = lane / 16, c = lane % 16;
+                    // 157 us with each lane storing its own row value by value, 32 in this way)
+                    if (lane == 0) tma_store_wait_read<0>();
+                    float* turned = (float*)(smem_raw + (piece - smem_u32(smem_raw)));
+                    const int r0 = lane / 16, c = lane % 16;
 #pragma unroll
                     for (int h = 0; h < 32; h += 16) {
+                        __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) piece[lane * 17 + j] = v[h + j];
+                        for (int j = 0; j < 16; ++j) turned[lane * 16 + ((j + lane) & 15)] = v[h + j];
                         __syncwarp();
                         const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0 + h + c;
                         if (n0 + c0 + h + c < o.N)
 #pragma unroll 4
-                            for (int r = r0; r < rows_in; r += 2) put_one(o, first + r * o.ldy, piece[r * 17 + c]);
-                        __syncwarp();
+                            for (int r = r0; r < rows_in; r += 2) put_one(o, first + r * o.ldy, turned[r * 16 + ((c + r) & 15)]);
                     }
                 }
             }
@@ -216,6 +241,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
             if (acc) acc_phase ^= 1;
             acc ^= 1;
         }
+        if (lane == 0) tma_store_wait();
+        __syncwarp();
     }
     if (!ok) drain_after_error();
     tc_fence_before_sync();
@@ -482,13 +509,25 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     }
     const int bn = p.N <= 64 ? 64 : p.N <= 128 ? 128 : 256;
     TilesArgs a;
-    a.out = o; a.tile_m = kTile; a.m_tiles = (int)((p.M + kTile - 1) / kTile); a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices;
-    a.err = d->err_dev;
-    a.stall = stall_bytes();
+    a.out = o; a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
+    // Rows of a tile: 128, or fewer where as many rounds of tiles then fill all SMs evenly.  (57600 x 512 x 256: 450 tiles of 128 rows are 3.04
+    // rounds of 148, the fourth nearly empty; tiles of 98 rows fill four.)
+    const int64_t most = ((p.M + kTile - 1) / kTile * a.n_tiles + d->sms - 1) / d->sms * d->sms / a.n_tiles;
+    a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
+    a.m_tiles = (int)((p.M + a.tile_m - 1) / a.tile_m);
+    CUtensorMap ty = {}, ty_rest = {};               // of 32 rows, and of the rows that a tile has beyond multiples of 32
+    if (o.wide) {
+        const uint64_t dims[2] = {(uint64_t)p.N, (uint64_t)p.M}, strides[1] = {(uint64_t)(p.M == 1 ? (p.N * size + 15) / 16 * 16 : p.ldy * size)};
+        const uint32_t box[2] = {(uint32_t)(kPieceRow / size), 32}, rest[2] = {box[0], (uint32_t)(a.tile_m % 32 ? a.tile_m % 32 : 32)};
+        const CUtensorMapDataType type = p.y_type == ST_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : p.y_type == ST_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+        if (!encode_tensor_map(&ty, type, CU_TENSOR_MAP_SWIZZLE_64B, p.y, 2, dims, strides, box, msg, sizeof msg, "y") ||
+            !encode_tensor_map(&ty_rest, type, CU_TENSOR_MAP_SWIZZLE_64B, p.y, 2, dims, strides, rest, msg, sizeof msg, "y"))
+            return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
+    }
     if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, bn, msg, sizeof msg, "w"))
         return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)a.m_tiles * a.n_tiles, d->sms));
-    const auto go = [&](auto kernel, size_t bytes) { return launch_early(pdl_enabled(), kernel, grid, dim3(kTilesThreads), bytes, s, tx, tw, a); };
+    const auto go = [&](auto kernel, size_t bytes) { return launch_early(pdl_enabled(), kernel, grid, dim3(kTilesThreads), bytes, s, tx, tw, ty, ty_rest, a); };
     e = bn == 64 ? go(int8_tiles_kernel<64>, TilesShape<64>::bytes) : bn == 128 ? go(int8_tiles_kernel<128>, TilesShape<128>::bytes)
                                                                                : go(int8_tiles_kernel<256>, TilesShape<256>::bytes);
     return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
