@@ -17,6 +17,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <mutex>
 
@@ -49,18 +50,50 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"((uint64_t)map), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
+// 32 lanes x 32 columns in two steps: the registers hold the values behind the wait, which names them so that nothing reads them before
+__device__ __forceinline__ void tmem_ld_issue(uint32_t taddr, float (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
+          "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]),
+          "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld(float (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]),
+          "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
+          "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+        :: "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 struct Out {
     void* y; int64_t ldy; int type, wide;       // wide: rows of y take whole 16-byte stores
-    const float *sx, *sw, *bias; int relu;
+    const float *sx, *sw, *bias; float least, one;
     int M, N;
 };
-__device__ __forceinline__ float finish(int acc, float sx, float sw, float bias, bool has_bias, int relu)
+// `least`: 0 with ReLU, else minus infinity; NaN (a token or channel that is not finite) stays NaN.  Without a bias 0 is added, which changes nothing.
+__device__ __forceinline__ float at_least(float y, float least) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(y), "f"(least)); return r; }
+__device__ __forceinline__ float finish(int acc, float sx, float sw, float bias, float least)
 {
-    float y = __fmul_rn(__fmul_rn((float)acc, sx), sw);
-    if (has_bias) y = __fadd_rn(y, bias);
-    return relu ? (y < 0.f ? 0.f : y) : y;      // NaN (a token or channel that is not finite) stays NaN
+    return at_least(__fadd_rn(__fmul_rn(__fmul_rn((float)acc, sx), sw), bias), least);
+}
+// Two of them, two fp32 operations to an instruction.  The sum is a multiplication by a factor that the assembler does not know (`one` is 1):
+// it fuses mul.rn.f32x2 and add.rn.f32x2, which are to be rounded one by one
+__device__ __forceinline__ void finish2(float& a, float& b, float sx, float sw_a, float sw_b, float bias_a, float bias_b, float least, float one)
+{
+    const float x = (float)__float_as_int(a), y = (float)__float_as_int(b);
+    asm("{\n\t.reg .b64 v, s, w, c, o;\n\t"
+        "mov.b64 v, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\tmov.b64 w, {%5, %6};\n\tmov.b64 c, {%7, %8};\n\tmov.b64 o, {%9, %9};\n\t"
+        "mul.rn.f32x2 v, v, s;\n\tmul.rn.f32x2 v, v, w;\n\tfma.rn.f32x2 v, v, o, c;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "=f"(a), "=f"(b) : "f"(x), "f"(y), "f"(sx), "f"(sw_a), "f"(sw_b), "f"(bias_a), "f"(bias_b), "f"(one));
+    a = at_least(a, least);
+    b = at_least(b, least);
 }
 __device__ __forceinline__ uint16_t round16(float y, int type)
 {
@@ -79,33 +112,49 @@ __device__ __forceinline__ void put_one(const Out& o, int64_t at, float y)
 }
 
 // ---- many tokens ------------------------------------------------------------------------------------------------
-constexpr int kTilesThreads = 384;              // producer, issuer, two idle warps (registers), eight that store
-// `stall`: 0; a test of the give-up path makes the first stage expect bytes that no copy delivers, so that the waits behind it run out
 constexpr int kPieceRow = 64, kPieceBytes = 32 * kPieceRow;        // what a warp stages at a time: 32 rows of 64 bytes
-struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices; unsigned int* err; uint32_t stall; };
+constexpr int kMaxStages = 8, kMaxResident = 16;                    // stages of the ring; slices of weights that stay in shared memory
+constexpr int kTilesSmem = 218 * 1024;                              // of a block, beside scales, bias and barriers
+// `resident`: all weights of the block's columns stay in shared memory and only tokens go through the ring; the launch's blocks are a multiple of
+// n_tiles, so that a block's tiles have the same columns.  `by_tile`: the groups that store take tiles in turn, otherwise the
+// first two take half of the columns of each.  `pieces`: staging buffers of a warp.  `stall`: 0; a test of the give-up path makes the first
+// stage expect bytes that no copy delivers, so that the waits behind it run out.
+struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices, stages, resident, by_tile, pieces; unsigned int* err; uint32_t stall; };
 
+// Up to 128 columns: four accumulators and three groups of four warps that store; 256 columns: two and two.  (Blocks of 256 columns read 12 KB of
+// operands per 128 cycles of multiplication, of 128 columns 8 KB per 64: shared memory's rate.)
 template <int BN>
 struct TilesShape {
-    static constexpr int stage_bytes = (kTile + BN) * kSlice, stages = (int)(192 * 1024 / stage_bytes) < 8 ? (int)(192 * 1024 / stage_bytes) : 8;
-    static constexpr size_t bytes = (size_t)stages * stage_bytes + 8 * kPieceBytes + kSmemAlign;
-    static constexpr int acc_cols = BN < 32 ? 32 : BN;
+    static constexpr int accs = BN == 256 ? 2 : 4, groups = BN == 256 ? 2 : 3, threads = 128 + 128 * groups, cols = accs * BN;
+    static constexpr int x_bytes = kTile * kSlice, w_bytes = BN * kSlice, staging = 4 * groups * kPieceBytes;
+    static int stages(int slices, bool resident, int pieces)
+    {
+        const int room = kTilesSmem - kSmemAlign - pieces * staging - (resident ? slices * w_bytes : 0);
+        return std::min(room / (resident ? x_bytes : x_bytes + w_bytes), kMaxStages);
+    }
+    static size_t bytes(int slices, int stages, bool resident, int pieces)
+    {
+        return kSmemAlign + pieces * staging + (size_t)stages * (resident ? x_bytes : x_bytes + w_bytes) + (resident ? (size_t)slices * w_bytes : 0);
+    }
 };
 
 template <int BN>
-__global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
+__global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
 {
     using Shape = TilesShape<BN>;
-    constexpr int S = Shape::stages;
     extern __shared__ uint8_t smem_raw[];
-    const uint32_t ring = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1);
-    __shared__ __align__(8) uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
+    const uint32_t staging = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1), ring = staging + a.pieces * Shape::staging;
+    const uint32_t stage_bytes = a.resident ? Shape::x_bytes : Shape::x_bytes + Shape::w_bytes, weights = ring + a.stages * stage_bytes;
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[Shape::accs], acc_empty[Shape::accs], w_full[kMaxResident];
     __shared__ uint32_t tmem_slot;
-    __shared__ __align__(16) float column[2][2][BN];         // per accumulator: scales and bias of its columns
+    // scales and bias of a tile's columns, for each group twice: a warp may be a tile ahead of the others of its group
+    __shared__ __align__(16) float column[Shape::groups][2][2][BN];
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), 2 * Shape::acc_cols);
+    if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), Shape::cols);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < S; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 8); }
+        for (int i = 0; i < kMaxStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+        for (int i = 0; i < Shape::accs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), a.by_tile ? 4 : 8); }
+        for (int i = 0; i < kMaxResident; ++i) mbar_init(smem_u32(&w_full[i]), 1);
         fence_barrier_init();
         prefetch_map(&tm_x); prefetch_map(&tm_w);
     }
@@ -121,85 +170,102 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
         uint32_t stage = 0, phase = 1;          // a fresh barrier's phase before the first counts as completed
         for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
             const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
+            const bool first = t == (int)blockIdx.x;
             for (int s = 0; s < a.slices; ++s) {
                 ok = mbar_wait(smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
                 if (!ok) break;
                 if (elect_one()) {
-                    const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * Shape::stage_bytes;
-                    mbar_expect_tx(bar, (a.tile_m + BN) * kSlice + (t == (int)blockIdx.x && s == 0 ? a.stall : 0u));
+                    const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * stage_bytes;
+                    mbar_expect_tx(bar, a.tile_m * kSlice + (a.resident ? 0 : Shape::w_bytes) + (first && s == 0 ? a.stall : 0u));
                     tma_load_2d(dst, &tm_x, bar, s * kSlice, m0);
-                    tma_load_2d(dst + kTile * kSlice, &tm_w, bar, s * kSlice, n0);
+                    if (!a.resident) tma_load_2d(dst + Shape::x_bytes, &tm_w, bar, s * kSlice, n0);
+                    else if (first) {
+                        mbar_expect_tx(smem_u32(&w_full[s]), Shape::w_bytes);
+                        tma_load_2d(weights + s * Shape::w_bytes, &tm_w, smem_u32(&w_full[s]), s * kSlice, n0);
+                    }
                 }
                 __syncwarp();
-                if (++stage == S) { stage = 0; phase ^= 1; }
+                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
             }
         }
     } else if (warp == 1) {                     // issuer
         constexpr uint32_t idesc = instr_desc_i8(kTile, BN);
         uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 1;
         for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            const bool first = t == (int)blockIdx.x;
             ok = mbar_wait(smem_u32(&acc_empty[acc]), acc_phase, a.err, kWaitDone);
             if (!ok) break;
             tc_fence_after_sync();
             for (int s = 0; s < a.slices; ++s) {
-                ok = mbar_wait(smem_u32(&full[stage]), phase, a.err, kWaitFull);
+                ok = mbar_wait(smem_u32(&full[stage]), phase, a.err, kWaitFull) && (!a.resident || !first || mbar_wait(smem_u32(&w_full[s]), 0, a.err, kWaitFull));
                 if (!ok) break;
                 tc_fence_after_sync();
                 if (elect_one()) {
-                    const uint32_t src = ring + stage * Shape::stage_bytes;
-                    const uint64_t da = smem_desc(src, 16, 1024), db = smem_desc(src + kTile * kSlice, 16, 1024);
+                    const uint32_t src = ring + stage * stage_bytes;
+                    const uint64_t da = smem_desc(src, 16, 1024), db = smem_desc(a.resident ? weights + s * Shape::w_bytes : src + Shape::x_bytes, 16, 1024);
 #pragma unroll
-                    for (int k = 0; k < kSlice / 32; ++k) umma_i8(tmem + acc * Shape::acc_cols, da + 2 * k, db + 2 * k, idesc, (s | k) != 0);
+                    for (int k = 0; k < kSlice / 32; ++k) umma_i8(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, (s | k) != 0);
                     umma_commit(smem_u32(&empty[stage]));
                     if (s == a.slices - 1) umma_commit(smem_u32(&acc_full[acc]));
                 }
                 __syncwarp();
-                if (++stage == S) { stage = 0; phase ^= 1; }
+                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
             }
-            if (acc) acc_phase ^= 1;
-            acc ^= 1;
+            if (++acc == Shape::accs) { acc = 0; acc_phase ^= 1; }
         }
-    } else if (warp >= 4) {                     // scale and store: warps 4..7 the lower half of the columns, 8..11 the upper
-        const int half = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * half;
+    } else if (warp >= 4 && (a.by_tile || warp < 12)) {         // scale and store
+        const int group = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * group;
+        const int c_begin = a.by_tile ? 0 : group * (BN / 2), c_most = a.by_tile ? BN : (group + 1) * (BN / 2);
         const Out& o = a.out;
-        uint32_t acc = 0, acc_phase = 0;
-        const uint32_t piece = ring + S * Shape::stage_bytes + (warp - 4) * kPieceBytes;
-        for (int t = (int)blockIdx.x; t < tiles; t += gridDim.x) {
+        const bool whole_end = o.N * (o.type == ST_F32 ? 4 : 2) % 16 == 0;       // TMA leaves out the 16-byte pieces beyond y, but not the rest of one that y ends in
+        const uint32_t area = staging + (warp - 4) * a.pieces * kPieceBytes;
+        uint32_t piece = area;
+        int index = 0, turn = 0;
+        for (int t = (int)blockIdx.x; t < tiles; t += gridDim.x, ++index) {
+            if (a.by_tile && index % Shape::groups != group) continue;
+            const int acc = index % Shape::accs, acc_phase = index / Shape::accs & 1;
+            float (&scales)[2][BN] = column[group][turn];
+            turn ^= 1;
             const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
             const int64_t row = (int64_t)m0 + quarter * 32 + lane;
             const bool mine = quarter * 32 + lane < a.tile_m && row < o.M;
             const float sx = mine ? o.sx[row] : 0.f;
-            for (int c = half * (BN / 2) + tid; c < (half + 1) * (BN / 2); c += 128) {
+            for (int c = c_begin + tid; c < c_most; c += 128) {
                 const bool in = n0 + c < o.N;
-                column[acc][0][c] = in ? o.sw[n0 + c] : 0.f;
-                column[acc][1][c] = in && o.bias ? o.bias[n0 + c] : 0.f;
+                scales[0][c] = in ? o.sw[n0 + c] : 0.f;
+                scales[1][c] = in && o.bias ? o.bias[n0 + c] : 0.f;
             }
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
             // a warp whose wait has given up goes on through the tiles without storing: the others wait for it above
             if (ok) ok = mbar_wait(smem_u32(&acc_full[acc]), acc_phase, a.err, kWaitDone);
             tc_fence_after_sync();
             const int rows_in = min(min(a.tile_m, o.M - m0) - quarter * 32, 32);       // of this warp's 32
-            // TMA leaves out the rows and the 16-byte pieces that lie beyond y, but not the rest of a piece that y ends in
-            const bool whole_end = o.N * (o.type == ST_F32 ? 4 : 2) % 16 == 0;
             const CUtensorMap* tm_out = a.tile_m - quarter * 32 >= 32 ? &tm_y : &tm_y_rest;
+            const uint32_t lanes = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
+            const int c_end = ok && rows_in > 0 ? min(c_most, o.N - n0) : 0;
+            float next[32];                     // the next 32 columns are on their way while 32 are scaled and stored
+            __syncwarp();
+            if (c_begin < c_end) tmem_ld_issue(lanes + c_begin, next);
 #pragma unroll 1
-            for (int c0 = half * (BN / 2); ok && c0 < (half + 1) * (BN / 2) && n0 + c0 < o.N && rows_in > 0; c0 += 32) {
+            for (int c0 = c_begin; c0 < c_end; c0 += 32) {
                 float v[32];
+                tmem_wait_ld(next);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = next[j];
                 __syncwarp();
-                tmem_ld_32x32(tmem + acc * Shape::acc_cols + ((uint32_t)(quarter * 32) << 16) + c0, v);
+                if (c0 + 32 < c_end) tmem_ld_issue(lanes + c0 + 32, next);
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
-                    const float4 sw = *(const float4*)&column[acc][0][c0 + j], b = *(const float4*)&column[acc][1][c0 + j];
-                    v[j] = finish(__float_as_int(v[j]), sx, sw.x, b.x, o.bias != nullptr, o.relu);
-                    v[j + 1] = finish(__float_as_int(v[j + 1]), sx, sw.y, b.y, o.bias != nullptr, o.relu);
-                    v[j + 2] = finish(__float_as_int(v[j + 2]), sx, sw.z, b.z, o.bias != nullptr, o.relu);
-                    v[j + 3] = finish(__float_as_int(v[j + 3]), sx, sw.w, b.w, o.bias != nullptr, o.relu);
+                    const float4 sw = *(const float4*)&scales[0][c0 + j], b = *(const float4*)&scales[1][c0 + j];
+                    finish2(v[j], v[j + 1], sx, sw.x, sw.y, b.x, b.y, o.least, o.one);
+                    finish2(v[j + 2], v[j + 3], sx, sw.z, sw.w, b.z, b.w, o.least, o.one);
                 }
                 if (o.wide && (whole_end || n0 + c0 + 32 <= o.N)) {
-                    // rows of 64 bytes, 16-byte pieces where TMA's 64-byte swizzle has them (no two lanes of a store in one bank), one copy
+                    // rows of 64 bytes, 16-byte pieces where TMA's 64-byte swizzle has them (no two lanes of a store in one bank), one copy.
+                    // (57600 x 512 x 256: 27 us with lanes storing their own rows, 18.5 with the warp storing from shared memory, 17.3 in this way)
                     const int passes = o.type == ST_F32 ? 2 : 1;
                     for (int h = 0; h < passes; ++h) {
-                        if (lane == 0) tma_store_wait_read<0>();
+                        if (lane == 0) { if (a.pieces == 2) tma_store_wait_read<1>(); else tma_store_wait_read<0>(); }
                         __syncwarp();
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
@@ -214,11 +280,15 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
                         }
                         fence_async_shared();
                         __syncwarp();
-                        if (lane == 0 && n0 + c0 + 16 * h < o.N) { tma_store_2d(tm_out, piece, n0 + c0 + 16 * h, m0 + quarter * 32); tma_store_commit(); }
+                        if (lane == 0) {
+                            if (n0 + c0 + 16 * h < o.N) tma_store_2d(tm_out, piece, n0 + c0 + 16 * h, m0 + quarter * 32);
+                            tma_store_commit();
+                        }
+                        if (a.pieces == 2) piece ^= area ^ (area + kPieceBytes);
                     }
                 } else {
                     // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
-                    // 157 us with each lane storing its own row value by value, 32 in this way)
+                    // 157 us with each lane storing its own row value by value, 30 in this way)
                     if (lane == 0) tma_store_wait_read<0>();
                     float* turned = (float*)(smem_raw + (piece - smem_u32(smem_raw)));
                     const int r0 = lane / 16, c = lane % 16;
@@ -238,8 +308,6 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
-            if (acc) acc_phase ^= 1;
-            acc ^= 1;
         }
         if (lane == 0) tma_store_wait();
         __syncwarp();
@@ -247,7 +315,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     if (!ok) drain_after_error();
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 2) tmem_dealloc(tmem, 2 * Shape::acc_cols);
+    if (warp == 2) tmem_dealloc(tmem, Shape::cols);
 }
 
 // ---- few tokens, or few tiles --------------------------------------------------------------------------------------
@@ -340,7 +408,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
                 if (a.splits == 1) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (mine && c0 + j < count) put_one(o, (int64_t)(m0 + c0 + j) * o.ldy + channel, finish(__float_as_int(v[j]), o.sx[m0 + c0 + j], sw, bias, o.bias != nullptr, o.relu));
+                        if (mine && c0 + j < count) put_one(o, (int64_t)(m0 + c0 + j) * o.ldy + channel, finish(__float_as_int(v[j]), o.sx[m0 + c0 + j], sw, bias, o.least));
                 } else {                        // every MMA has read its operands: the ring is free
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
@@ -362,7 +430,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
                 int sum = 0;
                 const uint32_t at = ring + (c * kTile + threadIdx.x) * 4;
                 for (int r = 0; r < a.splits; ++r) sum += load_cluster(at, r);
-                if (mine) put_one(o, (int64_t)(m0 + c) * o.ldy + channel, finish(sum, o.sx[m0 + c], sw, bias, o.bias != nullptr, o.relu));
+                if (mine) put_one(o, (int64_t)(m0 + c) * o.ldy + channel, finish(sum, o.sx[m0 + c], sw, bias, o.least));
             }
         }
         __syncwarp();
@@ -410,7 +478,7 @@ __global__ void __launch_bounds__(256) int8_plain_kernel(const int8_t* __restric
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int n = n0 + tx + 16 * j;
-            if (n < o.N) put_one(o, m * o.ldy + n, finish(acc[i][j], o.sx[m], o.sw[n], o.bias ? o.bias[n] : 0.f, o.bias != nullptr, o.relu));
+            if (n < o.N) put_one(o, m * o.ldy + n, finish(acc[i][j], o.sx[m], o.sw[n], o.bias ? o.bias[n] : 0.f, o.least));
         }
     }
 }
@@ -469,7 +537,7 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
         *(volatile unsigned int*)d->err = 0;
         return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of an earlier product gave up (code %u); its result is not complete", code);
     }
-    Out o = {p.y, p.ldy, p.y_type, 0, p.x_scale, p.w_scale, p.bias, p.relu, (int)p.M, (int)p.N};
+    Out o = {p.y, p.ldy, p.y_type, 0, p.x_scale, p.w_scale, p.bias, p.relu ? 0.f : -INFINITY, 1.f, (int)p.M, (int)p.N};
     const int64_t size = p.y_type == ST_F32 ? 4 : 2;
     o.wide = aligned(p.y, 16) && (p.M == 1 || p.ldy * size % 16 == 0);
     const bool tma = aligned(p.x, 16) && aligned(p.w, 16) && (p.M == 1 || p.ldx % 16 == 0) && (p.N == 1 || p.ldw % 16 == 0);
@@ -512,9 +580,28 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     a.out = o; a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
     // Rows of a tile: 128, or fewer where as many rounds of tiles then fill all SMs evenly.  (57600 x 512 x 256: 450 tiles of 128 rows are 3.04
     // rounds of 148, the fourth nearly empty; tiles of 98 rows fill four.)
-    const int64_t most = ((p.M + kTile - 1) / kTile * a.n_tiles + d->sms - 1) / d->sms * d->sms / a.n_tiles;
-    a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
+    const auto even_rows = [&](int64_t per_round) {
+        const int64_t rounds = ((p.M + kTile - 1) / kTile + per_round - 1) / per_round;
+        return (int)std::min<int64_t>(kTile, (p.M + rounds * per_round - 1) / (rounds * per_round));
+    };
+    const auto shape = [&](auto f) { return bn == 64 ? f(TilesShape<64>()) : bn == 128 ? f(TilesShape<128>()) : f(TilesShape<256>()); };
+    // The weights of a block's columns stay in shared memory where they leave room for three stages of tokens and a block has two tiles at least
+    const int64_t columns = d->sms / a.n_tiles;          // blocks that share the same weights
+    const int kept_stages = shape([&](auto q) { return q.stages(slices, true, 1); });
+    const char* res = getenv("ST_INT8_RES");
+    a.resident = slices <= kMaxResident && kept_stages >= 3 && columns * a.n_tiles * 10 >= d->sms * 9 && (p.M + kTile - 1) / kTile >= 2 * columns && !(res && res[0] == '0');
+    if (a.resident) a.tile_m = even_rows(columns);
+    else {
+        const int64_t rounds = ((p.M + kTile - 1) / kTile * a.n_tiles + d->sms - 1) / d->sms, most = rounds * d->sms / a.n_tiles;
+        a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
+    }
     a.m_tiles = (int)((p.M + a.tile_m - 1) / a.tile_m);
+    a.pieces = 1;
+    a.stages = a.resident ? kept_stages : shape([&](auto q) { return q.stages(slices, false, 1); });
+    const int with_two = shape([&](auto q) { return q.stages(slices, a.resident, 2); });
+    if (with_two >= (a.resident ? 3 : 4) && !(res && res[0] && res[1] && res[2] == '0')) { a.pieces = 2; a.stages = with_two; }
+    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles, blocks = std::min<int64_t>(tiles, a.resident ? columns * a.n_tiles : d->sms);
+    a.by_tile = tiles > blocks && !(res && res[0] && res[1] == '0');
     CUtensorMap ty = {}, ty_rest = {};               // of 32 rows, and of the rows that a tile has beyond multiples of 32
     if (o.wide) {
         const uint64_t dims[2] = {(uint64_t)p.N, (uint64_t)p.M}, strides[1] = {(uint64_t)(p.M == 1 ? (p.N * size + 15) / 16 * 16 : p.ldy * size)};
@@ -526,10 +613,10 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     }
     if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, bn, msg, sizeof msg, "w"))
         return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
-    const dim3 grid((unsigned)std::min<int64_t>((int64_t)a.m_tiles * a.n_tiles, d->sms));
-    const auto go = [&](auto kernel, size_t bytes) { return launch_early(pdl_enabled(), kernel, grid, dim3(kTilesThreads), bytes, s, tx, tw, ty, ty_rest, a); };
-    e = bn == 64 ? go(int8_tiles_kernel<64>, TilesShape<64>::bytes) : bn == 128 ? go(int8_tiles_kernel<128>, TilesShape<128>::bytes)
-                                                                               : go(int8_tiles_kernel<256>, TilesShape<256>::bytes);
+    const auto go = [&](auto kernel, int threads, size_t bytes) { return launch_early(pdl_enabled(), kernel, dim3((unsigned)blocks), dim3((unsigned)threads), bytes, s, tx, tw, ty, ty_rest, a); };
+    const size_t bytes = shape([&](auto q) { return q.bytes(slices, a.stages, a.resident, a.pieces); });
+    e = bn == 64 ? go(int8_tiles_kernel<64>, TilesShape<64>::threads, bytes) : bn == 128 ? go(int8_tiles_kernel<128>, TilesShape<128>::threads, bytes)
+                                                                                        : go(int8_tiles_kernel<256>, TilesShape<256>::threads, bytes);
     return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
 }
 
