@@ -50,26 +50,7 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"((uint64_t)map), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
-// 32 lanes x 32 columns in two steps: the registers hold the values behind the wait, which names them so that nothing reads them before
-__device__ __forceinline__ void tmem_ld_issue(uint32_t taddr, float (&v)[32])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
-          "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]),
-          "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
-        : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_wait_ld(float (&v)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]),
-          "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
-          "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
-        :: "memory");
-}
+__device__ __forceinline__ int std_min(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 struct Out {
@@ -114,46 +95,45 @@ __device__ __forceinline__ void put_one(const Out& o, int64_t at, float y)
 // ---- many tokens ------------------------------------------------------------------------------------------------
 constexpr int kPieceRow = 64, kPieceBytes = 32 * kPieceRow;        // what a warp stages at a time: 32 rows of 64 bytes
 constexpr int kMaxStages = 8, kMaxResident = 16;                    // stages of the ring; slices of weights that stay in shared memory
+constexpr int kMaxGroups = 4, kTilesThreads = 128 + 128 * kMaxGroups;     // producer, issuer, two that idle; groups that store
 constexpr int kTilesSmem = 218 * 1024;                              // of a block, beside scales, bias and barriers
-// `resident`: all weights of the block's columns stay in shared memory and only tokens go through the ring; the launch's blocks are a multiple of
-// n_tiles, so that a block's tiles have the same columns.  `by_tile`: the groups that store take tiles in turn, otherwise the
-// first two take half of the columns of each.  `pieces`: staging buffers of a warp.  `stall`: 0; a test of the give-up path makes the first
-// stage expect bytes that no copy delivers, so that the waits behind it run out.
-struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices, stages, resident, by_tile, pieces; unsigned int* err; uint32_t stall; };
+// `groups` of four warps scale and store, `slots` tiles at a time, each tile by groups / slots of them, which share its columns.  `resident`: all
+// weights of the block's columns stay in shared memory and only tokens go through the ring; the launch's blocks are a multiple of
+// n_tiles, so that a block's tiles have the same columns.  `stall`: 0; a test of the give-up path makes the first stage expect bytes that
+// no copy delivers, so that the waits behind it run out.
+struct TilesArgs { Out out; int tile_m, m_tiles, n_tiles, slices, stages, resident, groups, slots; unsigned int* err; uint32_t stall; };
 
-// Up to 128 columns: four accumulators and three groups of four warps that store; 256 columns: two and two.  (Blocks of 256 columns read 12 KB of
-// operands per 128 cycles of multiplication, of 128 columns 8 KB per 64: shared memory's rate.)
+// (Blocks of 256 columns read 12 KB of operands per 128 cycles of multiplication, of 128 columns 8 KB per 64: shared memory's rate.)
 template <int BN>
 struct TilesShape {
-    static constexpr int accs = BN == 256 ? 2 : 4, groups = BN == 256 ? 2 : 3, threads = 128 + 128 * groups, cols = accs * BN;
-    static constexpr int x_bytes = kTile * kSlice, w_bytes = BN * kSlice, staging = 4 * groups * kPieceBytes;
-    static int stages(int slices, bool resident, int pieces)
+    static constexpr int accs = BN == 256 ? 2 : 4, cols = accs * BN, x_bytes = kTile * kSlice, w_bytes = BN * kSlice;
+    static constexpr int bytes(int slices, int stages, bool resident, int groups)
     {
-        const int room = kTilesSmem - kSmemAlign - pieces * staging - (resident ? slices * w_bytes : 0);
-        return std::min(room / (resident ? x_bytes : x_bytes + w_bytes), kMaxStages);
+        return kSmemAlign + 4 * groups * kPieceBytes + stages * (resident ? x_bytes : x_bytes + w_bytes) + (resident ? slices * w_bytes : 0);
     }
-    static size_t bytes(int slices, int stages, bool resident, int pieces)
+    static constexpr int stages(int slices, bool resident, int groups)
     {
-        return kSmemAlign + pieces * staging + (size_t)stages * (resident ? x_bytes : x_bytes + w_bytes) + (resident ? (size_t)slices * w_bytes : 0);
+        return std::min((kTilesSmem - bytes(slices, 0, resident, groups)) / (resident ? x_bytes : x_bytes + w_bytes), kMaxStages);
     }
 };
 
 template <int BN>
-__global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
+__global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
 {
     using Shape = TilesShape<BN>;
     extern __shared__ uint8_t smem_raw[];
-    const uint32_t staging = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1), ring = staging + a.pieces * Shape::staging;
+    const uint32_t staging = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1), ring = staging + 4 * a.groups * kPieceBytes;
     const uint32_t stage_bytes = a.resident ? Shape::x_bytes : Shape::x_bytes + Shape::w_bytes, weights = ring + a.stages * stage_bytes;
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[Shape::accs], acc_empty[Shape::accs], w_full[kMaxResident];
     __shared__ uint32_t tmem_slot;
     // scales and bias of a tile's columns, for each group twice: a warp may be a tile ahead of the others of its group
-    __shared__ __align__(16) float column[Shape::groups][2][2][BN];
+    constexpr int kWidth = BN == 256 ? 128 : BN;            // of four groups; two have the room of four
+    __shared__ __align__(16) float column[kMaxGroups * 4 * kWidth];
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), Shape::cols);
     if (threadIdx.x == 0) {
         for (int i = 0; i < kMaxStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
-        for (int i = 0; i < Shape::accs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), a.by_tile ? 4 : 8); }
+        for (int i = 0; i < Shape::accs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 4 * std_min(a.groups / a.slots, BN / 32)); }
         for (int i = 0; i < kMaxResident; ++i) mbar_init(smem_u32(&w_full[i]), 1);
         fence_barrier_init();
         prefetch_map(&tm_x); prefetch_map(&tm_w);
@@ -213,18 +193,18 @@ __global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(
             }
             if (++acc == Shape::accs) { acc = 0; acc_phase ^= 1; }
         }
-    } else if (warp >= 4 && (a.by_tile || warp < 12)) {         // scale and store
+    } else if (warp >= 4) {                     // scale and store
         const int group = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * group;
-        const int c_begin = a.by_tile ? 0 : group * (BN / 2), c_most = a.by_tile ? BN : (group + 1) * (BN / 2);
+        const int shares = std_min(a.groups / a.slots, BN / 32), width = BN / shares, slot = group / shares, c_begin = group % shares * width, c_most = c_begin + width;
         const Out& o = a.out;
         const bool whole_end = o.N * (o.type == ST_F32 ? 4 : 2) % 16 == 0;       // TMA leaves out the 16-byte pieces beyond y, but not the rest of one that y ends in
-        const uint32_t area = staging + (warp - 4) * a.pieces * kPieceBytes;
-        uint32_t piece = area;
+        const uint32_t piece = staging + (warp - 4) * kPieceBytes;
+        float* const columns = column + group * 4 * (a.groups == 2 && BN == 256 ? 256 : kWidth);
         int index = 0, turn = 0;
         for (int t = (int)blockIdx.x; t < tiles; t += gridDim.x, ++index) {
-            if (a.by_tile && index % Shape::groups != group) continue;
+            if (index % a.slots != slot) continue;
             const int acc = index % Shape::accs, acc_phase = index / Shape::accs & 1;
-            float (&scales)[2][BN] = column[group][turn];
+            float *const scales = columns + turn * 2 * width - c_begin, *const biases = scales + width;       // of column c at [c]
             turn ^= 1;
             const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
             const int64_t row = (int64_t)m0 + quarter * 32 + lane;
@@ -232,8 +212,8 @@ __global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(
             const float sx = mine ? o.sx[row] : 0.f;
             for (int c = c_begin + tid; c < c_most; c += 128) {
                 const bool in = n0 + c < o.N;
-                scales[0][c] = in ? o.sw[n0 + c] : 0.f;
-                scales[1][c] = in && o.bias ? o.bias[n0 + c] : 0.f;
+                scales[c] = in ? o.sw[n0 + c] : 0.f;
+                biases[c] = in && o.bias ? o.bias[n0 + c] : 0.f;
             }
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
             // a warp whose wait has given up goes on through the tiles without storing: the others wait for it above
@@ -243,20 +223,14 @@ __global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(
             const CUtensorMap* tm_out = a.tile_m - quarter * 32 >= 32 ? &tm_y : &tm_y_rest;
             const uint32_t lanes = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
             const int c_end = ok && rows_in > 0 ? min(c_most, o.N - n0) : 0;
-            float next[32];                     // the next 32 columns are on their way while 32 are scaled and stored
-            __syncwarp();
-            if (c_begin < c_end) tmem_ld_issue(lanes + c_begin, next);
 #pragma unroll 1
             for (int c0 = c_begin; c0 < c_end; c0 += 32) {
                 float v[32];
-                tmem_wait_ld(next);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = next[j];
                 __syncwarp();
-                if (c0 + 32 < c_end) tmem_ld_issue(lanes + c0 + 32, next);
+                tmem_ld_32x32(lanes + c0, v);
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
-                    const float4 sw = *(const float4*)&scales[0][c0 + j], b = *(const float4*)&scales[1][c0 + j];
+                    const float4 sw = *(const float4*)(scales + c0 + j), b = *(const float4*)(biases + c0 + j);
                     finish2(v[j], v[j + 1], sx, sw.x, sw.y, b.x, b.y, o.least, o.one);
                     finish2(v[j + 2], v[j + 3], sx, sw.z, sw.w, b.z, b.w, o.least, o.one);
                 }
@@ -265,7 +239,7 @@ __global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(
                     // (57600 x 512 x 256: 27 us with lanes storing their own rows, 18.5 with the warp storing from shared memory, 17.3 in this way)
                     const int passes = o.type == ST_F32 ? 2 : 1;
                     for (int h = 0; h < passes; ++h) {
-                        if (lane == 0) { if (a.pieces == 2) tma_store_wait_read<1>(); else tma_store_wait_read<0>(); }
+                        if (lane == 0) tma_store_wait_read<0>();
                         __syncwarp();
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
@@ -284,7 +258,6 @@ __global__ void __launch_bounds__(TilesShape<BN>::threads, 1) int8_tiles_kernel(
                             if (n0 + c0 + 16 * h < o.N) tma_store_2d(tm_out, piece, n0 + c0 + 16 * h, m0 + quarter * 32);
                             tma_store_commit();
                         }
-                        if (a.pieces == 2) piece ^= area ^ (area + kPieceBytes);
                     }
                 } else {
                     // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
@@ -587,21 +560,20 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     const auto shape = [&](auto f) { return bn == 64 ? f(TilesShape<64>()) : bn == 128 ? f(TilesShape<128>()) : f(TilesShape<256>()); };
     // The weights of a block's columns stay in shared memory where they leave room for three stages of tokens and a block has two tiles at least
     const int64_t columns = d->sms / a.n_tiles;          // blocks that share the same weights
-    const int kept_stages = shape([&](auto q) { return q.stages(slices, true, 1); });
-    const char* res = getenv("ST_INT8_RES");
-    a.resident = slices <= kMaxResident && kept_stages >= 3 && columns * a.n_tiles * 10 >= d->sms * 9 && (p.M + kTile - 1) / kTile >= 2 * columns && !(res && res[0] == '0');
+    const int kept_stages = shape([&](auto q) { return q.stages(slices, true, kMaxGroups); });
+    a.resident = slices <= kMaxResident && kept_stages >= 3 && columns * a.n_tiles * 10 >= d->sms * 9 && (p.M + kTile - 1) / kTile >= 2 * columns;
     if (a.resident) a.tile_m = even_rows(columns);
     else {
         const int64_t rounds = ((p.M + kTile - 1) / kTile * a.n_tiles + d->sms - 1) / d->sms, most = rounds * d->sms / a.n_tiles;
         a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
     }
     a.m_tiles = (int)((p.M + a.tile_m - 1) / a.tile_m);
-    a.pieces = 1;
-    a.stages = a.resident ? kept_stages : shape([&](auto q) { return q.stages(slices, false, 1); });
-    const int with_two = shape([&](auto q) { return q.stages(slices, a.resident, 2); });
-    if (with_two >= (a.resident ? 3 : 4) && !(res && res[0] && res[1] && res[2] == '0')) { a.pieces = 2; a.stages = with_two; }
+    // Four groups that store where their staging leaves the ring four stages (three beside resident weights), else two
+    a.groups = kMaxGroups;
+    a.stages = a.resident ? kept_stages : shape([&](auto q) { return q.stages(slices, false, kMaxGroups); });
+    if (!a.resident && a.stages < 4) { a.groups = 2; a.stages = shape([&](auto q) { return q.stages(slices, false, 2); }); }
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles, blocks = std::min<int64_t>(tiles, a.resident ? columns * a.n_tiles : d->sms);
-    a.by_tile = tiles > blocks && !(res && res[0] && res[1] == '0');
+    a.slots = tiles <= blocks ? 1 : shape([&](auto q) { return std::min(a.groups, q.accs); });
     CUtensorMap ty = {}, ty_rest = {};               // of 32 rows, and of the rows that a tile has beyond multiples of 32
     if (o.wide) {
         const uint64_t dims[2] = {(uint64_t)p.N, (uint64_t)p.M}, strides[1] = {(uint64_t)(p.M == 1 ? (p.N * size + 15) / 16 * 16 : p.ldy * size)};
@@ -613,10 +585,9 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     }
     if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, bn, msg, sizeof msg, "w"))
         return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
-    const auto go = [&](auto kernel, int threads, size_t bytes) { return launch_early(pdl_enabled(), kernel, dim3((unsigned)blocks), dim3((unsigned)threads), bytes, s, tx, tw, ty, ty_rest, a); };
-    const size_t bytes = shape([&](auto q) { return q.bytes(slices, a.stages, a.resident, a.pieces); });
-    e = bn == 64 ? go(int8_tiles_kernel<64>, TilesShape<64>::threads, bytes) : bn == 128 ? go(int8_tiles_kernel<128>, TilesShape<128>::threads, bytes)
-                                                                                        : go(int8_tiles_kernel<256>, TilesShape<256>::threads, bytes);
+    const size_t bytes = shape([&](auto q) { return (size_t)q.bytes(slices, a.stages, a.resident, a.groups); });
+    const auto go = [&](auto kernel) { return launch_early(pdl_enabled(), kernel, dim3((unsigned)blocks), dim3(128 + 128 * a.groups), bytes, s, tx, tw, ty, ty_rest, a); };
+    e = bn == 64 ? go(int8_tiles_kernel<64>) : bn == 128 ? go(int8_tiles_kernel<128>) : go(int8_tiles_kernel<256>);
     return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
 }
 
