@@ -117,6 +117,30 @@ struct TilesShape {
     }
 };
 
+// A warp's 32 rows x 32 columns (a row to a lane) to y by TMA: staged in rows of 64 bytes, their 16-byte pieces where TMA's 64-byte swizzle has them
+template <int TYPE>
+__device__ __forceinline__ void stage_and_store(const float (&v)[32], uint32_t piece, int lane, const CUtensorMap* map, int col, int row, int N)
+{
+#pragma unroll
+    for (int h = 0; h < (TYPE == ST_F32 ? 2 : 1); ++h) {
+        if (lane == 0) tma_store_wait_read<0>();
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t to = piece + lane * kPieceRow + ((k ^ ((lane >> 1) & 3)) * 16);
+            const float* x = v + (TYPE == ST_F32 ? 16 * h + 4 * k : 8 * k);
+            if (TYPE == ST_F32) st_shared_128(to, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+            else st_shared_128(to, round16x2(x[0], x[1], TYPE), round16x2(x[2], x[3], TYPE), round16x2(x[4], x[5], TYPE), round16x2(x[6], x[7], TYPE));
+        }
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+            if (col + 16 * h < N) tma_store_2d(map, piece, col + 16 * h, row);
+            tma_store_commit();
+        }
+    }
+}
+
 template <int BN>
 __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
 {
@@ -235,30 +259,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
                     finish2(v[j + 2], v[j + 3], sx, sw.z, sw.w, b.z, b.w, o.least, o.one);
                 }
                 if (o.wide && (whole_end || n0 + c0 + 32 <= o.N)) {
-                    // rows of 64 bytes, 16-byte pieces where TMA's 64-byte swizzle has them (no two lanes of a store in one bank), one copy.
                     // (57600 x 512 x 256: 27 us with lanes storing their own rows, 18.5 with the warp storing from shared memory, 17.3 in this way)
-                    const int passes = o.type == ST_F32 ? 2 : 1;
-                    for (int h = 0; h < passes; ++h) {
-                        if (lane == 0) tma_store_wait_read<0>();
-                        __syncwarp();
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t to = piece + lane * kPieceRow + ((k ^ ((lane >> 1) & 3)) * 16);
-                            if (o.type == ST_F32) {
-                                const float *lo = v + 4 * k, *hi = v + 16 + 4 * k;
-                                st_shared_128(to, __float_as_uint(h ? hi[0] : lo[0]), __float_as_uint(h ? hi[1] : lo[1]), __float_as_uint(h ? hi[2] : lo[2]), __float_as_uint(h ? hi[3] : lo[3]));
-                            } else {
-                                st_shared_128(to, round16x2(v[8 * k], v[8 * k + 1], o.type), round16x2(v[8 * k + 2], v[8 * k + 3], o.type),
-                                              round16x2(v[8 * k + 4], v[8 * k + 5], o.type), round16x2(v[8 * k + 6], v[8 * k + 7], o.type));
-                            }
-                        }
-                        fence_async_shared();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (n0 + c0 + 16 * h < o.N) tma_store_2d(tm_out, piece, n0 + c0 + 16 * h, m0 + quarter * 32);
-                            tma_store_commit();
-                        }
-                    }
+                    const int at_row = m0 + quarter * 32, at_col = n0 + c0;
+                    if (o.type == ST_BF16) stage_and_store<ST_BF16>(v, piece, lane, tm_out, at_col, at_row, o.N);
+                    else if (o.type == ST_F16) stage_and_store<ST_F16>(v, piece, lane, tm_out, at_col, at_row, o.N);
+                    else stage_and_store<ST_F32>(v, piece, lane, tm_out, at_col, at_row, o.N);
                 } else {
                     // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
                     // 157 us with each lane storing its own row value by value, 30 in this way)
@@ -272,9 +277,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
                         for (int j = 0; j < 16; ++j) turned[lane * 16 + ((j + lane) & 15)] = v[h + j];
                         __syncwarp();
                         const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0 + h + c;
-                        if (n0 + c0 + h + c < o.N)
-#pragma unroll 4
-                            for (int r = r0; r < rows_in; r += 2) put_one(o, first + r * o.ldy, turned[r * 16 + ((c + r) & 15)]);
+                        if (n0 + c0 + h + c >= o.N) continue;
+                        if (o.type == ST_F32) {
+#pragma unroll 8
+                            for (int r = r0; r < rows_in; r += 2) ((float*)o.y)[first + r * o.ldy] = turned[r * 16 + ((c + r) & 15)];
+                        } else {
+#pragma unroll 8
+                            for (int r = r0; r < rows_in; r += 2) ((uint16_t*)o.y)[first + r * o.ldy] = round16(turned[r * 16 + ((c + r) & 15)], o.type);
+                        }
                     }
                 }
             }
