@@ -170,15 +170,17 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     pdl_launch_dependents();
     const int tiles = a.m_tiles * a.n_tiles;
     bool ok = true;
+    // Producer and issuer are one thread each that looks at the next barrier before it waits for this one's (as whole warps that vote and
+    // elect they took 500 cycles a slice, whatever its width)
     if (warp == 0) {                            // producer
-        uint32_t stage = 0, phase = 1;          // a fresh barrier's phase before the first counts as completed
-        for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
-            const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
-            const bool first = t == (int)blockIdx.x;
-            for (int s = 0; s < a.slices; ++s) {
-                ok = mbar_wait(smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
-                if (!ok) break;
-                if (elect_one()) {
+        if (elect_one()) {
+            uint32_t stage = 0, phase = 1;      // a fresh barrier's phase before the first counts as completed
+            for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
+                const bool first = t == (int)blockIdx.x;
+                for (int s = 0; s < a.slices; ++s) {
+                    ok = mbar_wait_from(false, smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
+                    if (!ok) break;
                     const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * stage_bytes;
                     mbar_expect_tx(bar, a.tile_m * kSlice + (a.resident ? 0 : Shape::w_bytes) + (first && s == 0 ? a.stall : 0u));
                     tma_load_2d(dst, &tm_x, bar, s * kSlice, m0);
@@ -187,36 +189,40 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
                         mbar_expect_tx(smem_u32(&w_full[s]), Shape::w_bytes);
                         tma_load_2d(weights + s * Shape::w_bytes, &tm_w, smem_u32(&w_full[s]), s * kSlice, n0);
                     }
+                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
                 }
-                __syncwarp();
-                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
             }
         }
+        __syncwarp();
     } else if (warp == 1) {                     // issuer
-        constexpr uint32_t idesc = instr_desc_i8(kTile, BN);
-        uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 1;
-        for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
-            const bool first = t == (int)blockIdx.x;
-            ok = mbar_wait(smem_u32(&acc_empty[acc]), acc_phase, a.err, kWaitDone);
-            if (!ok) break;
-            tc_fence_after_sync();
-            for (int s = 0; s < a.slices; ++s) {
-                ok = mbar_wait(smem_u32(&full[stage]), phase, a.err, kWaitFull) && (!a.resident || !first || mbar_wait(smem_u32(&w_full[s]), 0, a.err, kWaitFull));
+        if (elect_one()) {
+            constexpr uint32_t idesc = instr_desc_i8(kTile, BN);
+            const uint64_t desc0 = smem_desc(ring, 16, 1024), w_desc0 = smem_desc(a.resident ? weights : ring + Shape::x_bytes, 16, 1024);
+            const uint32_t step = stage_bytes >> 4, w_step = a.resident ? Shape::w_bytes >> 4 : step;
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 1;
+            bool ready = false;                 // the next stage's data has been seen to be there
+            for (int t = (int)blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                const bool first = t == (int)blockIdx.x;
+                ok = mbar_wait_from(false, smem_u32(&acc_empty[acc]), acc_phase, a.err, kWaitDone);
                 if (!ok) break;
-                tc_fence_after_sync();
-                if (elect_one()) {
-                    const uint32_t src = ring + stage * stage_bytes;
-                    const uint64_t da = smem_desc(src, 16, 1024), db = smem_desc(a.resident ? weights + s * Shape::w_bytes : src + Shape::x_bytes, 16, 1024);
+                for (int s = 0; s < a.slices; ++s) {
+                    ok = mbar_wait_from(ready, smem_u32(&full[stage]), phase, a.err, kWaitFull) && (!a.resident || !first || mbar_wait_from(false, smem_u32(&w_full[s]), 0, a.err, kWaitFull));
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t now = stage;
+                    if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                    ready = mbar_try_wait(smem_u32(&full[stage]), phase);
+                    const uint64_t da = desc0 + now * step, db = w_desc0 + (a.resident ? (uint32_t)s : now) * w_step;
 #pragma unroll
                     for (int k = 0; k < kSlice / 32; ++k) umma_i8(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, (s | k) != 0);
-                    umma_commit(smem_u32(&empty[stage]));
-                    if (s == a.slices - 1) umma_commit(smem_u32(&acc_full[acc]));
+                    umma_commit(smem_u32(&empty[now]));
                 }
-                __syncwarp();
-                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                if (!ok) break;
+                umma_commit(smem_u32(&acc_full[acc]));
+                if (++acc == Shape::accs) { acc = 0; acc_phase ^= 1; }
             }
-            if (++acc == Shape::accs) { acc = 0; acc_phase ^= 1; }
         }
+        __syncwarp();
     } else if (warp >= 4) {                     // scale and store
         const int group = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * group;
         const int shares = std_min(a.groups / a.slots, BN / 32), width = BN / shares, slot = group / shares, c_begin = group % shares * width, c_most = c_begin + width;
@@ -303,16 +309,31 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
 
 // ---- few tokens, or few tiles --------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 192;              // four warps that store, producer, issuer
-constexpr int kMaxSplitStages = 8;
+constexpr int kMaxSplitStages = 8, kMaxSplits = 8;
 struct SplitArgs { Out out; int slices, splits, stages; unsigned int* err; uint32_t stall; };
 
 __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ int load_cluster(uint32_t addr, uint32_t rank)
+__device__ __forceinline__ int4 load_cluster(uint32_t addr, uint32_t rank)
 {
-    uint32_t at; int v;
+    uint32_t at; int4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
+}
+// Four channels of a token; where rows of y are aligned and hold all four, one store
+__device__ __forceinline__ void put_four(const Out& o, int64_t token, int channel, const int4& acc, float sx, const float4& sw, const float4& bias)
+{
+    const float y[4] = {finish(acc.x, sx, sw.x, bias.x, o.least), finish(acc.y, sx, sw.y, bias.y, o.least), finish(acc.z, sx, sw.z, bias.z, o.least),
+                        finish(acc.w, sx, sw.w, bias.w, o.least)};
+    const int64_t at = token * o.ldy + channel;
+    if (o.wide && channel + 4 <= o.N) {
+        if (o.type == ST_F32) *(float4*)((float*)o.y + at) = make_float4(y[0], y[1], y[2], y[3]);
+        else *(uint2*)((uint16_t*)o.y + at) = make_uint2(round16x2(y[0], y[1], o.type), round16x2(y[2], y[3], o.type));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (channel + j < o.N) put_one(o, at + j, y[j]);
+    }
 }
 
 // Block r of a cluster of `splits` sums slices [r, r + 1) / splits of K for 128 channels x BT tokens; sums are whole numbers, so their order does not
@@ -345,36 +366,40 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
     bool ok = true;
     const int count = min(o.M - m0, BT);        // tokens of the tile
     if (warp == 4) {
-        uint32_t stage = 0, phase = 1;
-        for (int s = begin; s < end; ++s) {
-            ok = mbar_wait(smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
-            if (!ok) break;
-            if (elect_one()) {
+        if (elect_one()) {
+            uint32_t stage = 0, phase = 1;
+            for (int s = begin; s < end; ++s) {
+                ok = mbar_wait_from(false, smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
+                if (!ok) break;
                 const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * kStage;
                 mbar_expect_tx(bar, kStage + (s == begin ? a.stall : 0u));
                 tma_load_2d(dst, &tm_w, bar, s * kSlice, n0);
                 tma_load_2d(dst + kTile * kSlice, &tm_x, bar, s * kSlice, m0);
+                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
             }
-            __syncwarp();
-            if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
         }
+        __syncwarp();
     } else if (warp == 5) {
-        constexpr uint32_t idesc = instr_desc_i8(kTile, BT);
-        uint32_t stage = 0, phase = 0;
-        for (int s = begin; s < end; ++s) {
-            ok = mbar_wait(smem_u32(&full[stage]), phase, a.err, kWaitFull);
-            if (!ok) break;
-            tc_fence_after_sync();
-            if (elect_one()) {
-                const uint32_t src = ring + stage * kStage;
-                const uint64_t da = smem_desc(src, 16, 1024), db = smem_desc(src + kTile * kSlice, 16, 1024);
+        if (elect_one()) {
+            constexpr uint32_t idesc = instr_desc_i8(kTile, BT);
+            const uint64_t desc0 = smem_desc(ring, 16, 1024);
+            uint32_t stage = 0, phase = 0;
+            bool ready = false;
+            for (int s = begin; s < end; ++s) {
+                ok = mbar_wait_from(ready, smem_u32(&full[stage]), phase, a.err, kWaitFull);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t now = stage;
+                if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+                ready = mbar_try_wait(smem_u32(&full[stage]), phase);
+                const uint64_t da = desc0 + now * (kStage >> 4), db = da + (kTile * kSlice >> 4);
 #pragma unroll
                 for (int k = 0; k < kSlice / 32; ++k) umma_i8(tmem, da + 2 * k, db + 2 * k, idesc, (s != begin) | (k != 0));
-                umma_commit(smem_u32(s == end - 1 ? &acc_full : &empty[stage]));
+                umma_commit(smem_u32(&empty[now]));
             }
-            __syncwarp();
-            if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
+            if (ok) umma_commit(smem_u32(&acc_full));
         }
+        __syncwarp();
     } else if (warp < 4) {
         const int channel = n0 + threadIdx.x;
         const bool mine = channel < o.N;
@@ -406,14 +431,24 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
         const int all_ok = __syncthreads_and(ok);
         cluster_sync();
         if (warp < 4 && all_ok) {
-            const int channel = n0 + threadIdx.x;
-            const bool mine = channel < o.N;
-            const float sw = mine ? o.sw[channel] : 0.f, bias = mine && o.bias ? o.bias[channel] : 0.f;
-            for (int c = split; c < count; c += a.splits) {
-                int sum = 0;
-                const uint32_t at = ring + (c * kTile + threadIdx.x) * 4;
-                for (int r = 0; r < a.splits; ++r) sum += load_cluster(at, r);
-                if (mine) put_one(o, (int64_t)(m0 + c) * o.ldy + channel, finish(sum, o.sx[m0 + c], sw, bias, o.least));
+            // a warp to a token, four channels to a lane; the sums of all blocks are on their way together
+            const int channel = n0 + 4 * lane;
+            float scales[4], biases[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                scales[j] = channel + j < o.N ? o.sw[channel + j] : 0.f;
+                biases[j] = channel + j < o.N && o.bias ? o.bias[channel + j] : 0.f;
+            }
+            const float4 sw = make_float4(scales[0], scales[1], scales[2], scales[3]), bias = make_float4(biases[0], biases[1], biases[2], biases[3]);
+            for (int c = split + a.splits * warp; c < count; c += 4 * a.splits) {
+                const uint32_t at = ring + (c * kTile + 4 * lane) * 4;
+                int4 part[kMaxSplits];
+#pragma unroll
+                for (int r = 0; r < kMaxSplits; ++r) part[r] = r < a.splits ? load_cluster(at, r) : make_int4(0, 0, 0, 0);
+                int4 sum = part[0];
+#pragma unroll
+                for (int r = 1; r < kMaxSplits; ++r) { sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w; }
+                put_four(o, m0 + c, channel, sum, o.sx[m0 + c], sw, bias);
             }
         }
         __syncwarp();
@@ -538,7 +573,7 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
         const int64_t m_tiles = (p.M + bt - 1) / bt, n_tiles = (p.N + kTile - 1) / kTile;
         int splits = 1;
         while (splits < 8 && m_tiles * n_tiles * splits * 2 <= d->sms + 20 && slices >= splits * 2) splits *= 2;
-        if (form && form[1]) splits = form[1] - '0';
+        if (form && form[1]) splits = std::min(form[1] - '0', slices >= 8 ? 8 : slices >= 4 ? 4 : slices >= 2 ? 2 : 1);
         SplitArgs a;
         a.out = o; a.slices = slices; a.splits = splits; a.err = d->err_dev; a.stall = stall_bytes();
         const int stage = (kTile + bt) * kSlice, per = (slices + splits - 1) / splits;
@@ -558,7 +593,7 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
           : bt == 64 ? cudaLaunchKernelEx(&cfg, int8_split_kernel<64>, tx, tw, a) : cudaLaunchKernelEx(&cfg, int8_split_kernel<128>, tx, tw, a);
         return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
     }
-    const int bn = p.N <= 64 ? 64 : p.N <= 128 ? 128 : 256;
+    const int bn = getenv("ST_INT8_BN") ? atoi(getenv("ST_INT8_BN")) : p.N <= 64 ? 64 : p.N <= 128 ? 128 : 256;
     TilesArgs a;
     a.out = o; a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
     // Rows of a tile: 128, or fewer where as many rounds of tiles then fill all SMs evenly.  (57600 x 512 x 256: 450 tiles of 128 rows are 3.04
