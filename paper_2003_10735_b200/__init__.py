@@ -9,6 +9,7 @@ no fallback: if the CUDA library has not been built the first call raises.
 from __future__ import annotations
 
 import ctypes
+import itertools
 import os
 from typing import Optional
 
@@ -213,14 +214,16 @@ def _ptr(buf, dtype: str, min_elems: int, what: str) -> Optional[int]:
         kind, address = buf.dtype, buf.data_ptr
     except AttributeError:
         raise TypeError(f"{what}: expected a torch tensor or numpy array") from None
-    name = _NAME_OF.get(kind)
-    if name is None:
-        name = _NAME_OF[kind] = str(kind).removeprefix("torch.")
-    if name != dtype or not buf.is_contiguous():
+    if (_NAME_OF.get(kind) or _name_of(kind)) != dtype or not buf.is_contiguous():
         raise TypeError(f"{what}: need a contiguous {dtype} tensor, got {buf.dtype}")
     if buf.numel() < min_elems:
         raise ValueError(f"{what}: {buf.numel()} elements, need {min_elems}")
     return address()
+
+
+def _name_of(kind) -> str:
+    name = _NAME_OF[kind] = str(kind).removeprefix("torch.")
+    return name
 
 
 class _Ctx:
@@ -430,13 +433,13 @@ def st_measure_arithmetic_peaks(cuda_stream: int = 0):
 # ---------------------------------------------------------------------------- 8-bit integer layers of the frozen part
 def _matrix(t, names, what: str):
     """(address, element type's name, rows, columns, row pitch) of a CUDA matrix whose rows are contiguous."""
-    name = str(t.dtype).removeprefix("torch.")
+    name, shape, strides = _NAME_OF.get(t.dtype) or _name_of(t.dtype), t.shape, t.stride()
     if name not in names:
         raise TypeError(f"{what}: need {' or '.join(names)}, got {t.dtype}")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TypeError(f"{what}: need a matrix whose rows are contiguous, got shape {tuple(t.shape)} with strides {t.stride()}")
-    rows, cols = t.shape
-    return t.data_ptr(), name, rows, cols, t.stride(0) if rows > 1 else max(cols, 1)
+    if len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
+        raise TypeError(f"{what}: need a matrix whose rows are contiguous, got shape {tuple(shape)} with strides {strides}")
+    rows, cols = shape
+    return t.data_ptr(), name, rows, cols, strides[0] if rows > 1 else cols or 1
 
 
 def st_quantize_rows(x, q, scale, cuda_stream: int = 0) -> None:
@@ -445,16 +448,20 @@ def st_quantize_rows(x, q, scale, cuda_stream: int = 0) -> None:
     name = _dtype_name(x, "x")
     if x.dim() != 2:
         raise TypeError(f"x: need a matrix, got shape {tuple(x.shape)}")
-    address, _, rows, cols, ldq = _matrix(q, ("int8",), "q")
-    if (rows, cols) != tuple(x.shape):
-        raise ValueError(f"q: shape {(rows, cols)}, need {tuple(x.shape)}")
-    _check(load_library().st_quantize_rows(x.data_ptr(), _TYPE_OF[name], rows, cols, x.stride(0), x.stride(1), address, ldq,
-                                           _ptr(scale, "float32", rows, "scale"), cuda_stream or None), None)
+    address, _, rows, cols, ldq = _matrix(q, _INT8, "q")
+    shape, strides = x.shape, x.stride()
+    if rows != shape[0] or cols != shape[1]:
+        raise ValueError(f"q: shape {(rows, cols)}, need {tuple(shape)}")
+    _check((_lib or load_library()).st_quantize_rows(x.data_ptr(), _TYPE_OF[name], rows, cols, strides[0], strides[1], address, ldq,
+                                                     _ptr(scale, "float32", rows, "scale"), cuda_stream or None), None)
+
+
+_INT8 = ("int8",)
 
 
 def _int8_operands(x, x_scale, w, w_scale, bias):
-    xa, _, m, k, ldx = _matrix(x, ("int8",), "x")
-    wa, _, n, kw, ldw = _matrix(w, ("int8",), "w")
+    xa, _, m, k, ldx = _matrix(x, _INT8, "x")
+    wa, _, n, kw, ldw = _matrix(w, _INT8, "w")
     if k != kw:
         raise ValueError(f"w: {kw} columns, x has {k}")
     return (xa, ldx, _ptr(x_scale, "float32", m, "x_scale"), wa, ldw, _ptr(w_scale, "float32", n, "w_scale"), _ptr(bias, "float32", n, "bias")), m, n, k
@@ -464,10 +471,10 @@ def st_int8_matmul(x, x_scale, w, w_scale, y, bias=None, relu: bool = False, cud
     """y[m][n] = act((sum_k x[m][k] w[n][k]) x_scale[m] w_scale[n] + bias[n]); x, w int8 and y float32, bfloat16 or float16, CUDA matrices
     whose rows are contiguous (rows of x and w at multiples of 16 bytes run on tensor cores)."""
     operands, m, n, k = _int8_operands(x, x_scale, w, w_scale, bias)
-    ya, name, my, ny, ldy = _matrix(y, tuple(_TYPE_OF), "y")
-    if (my, ny) != (m, n):
+    ya, name, my, ny, ldy = _matrix(y, _TYPE_OF, "y")
+    if my != m or ny != n:
         raise ValueError(f"y: shape {(my, ny)}, need {(m, n)}")
-    _check(load_library().st_int8_matmul(*operands, int(relu), m, n, k, ya, _TYPE_OF[name], ldy, cuda_stream or None), None)
+    _check((_lib or load_library()).st_int8_matmul(*operands, int(relu), m, n, k, ya, _TYPE_OF[name], ldy, cuda_stream or None), None)
 
 
 def st_set_frozen_features_int8(ctx: _Ctx, stream: int, x, x_scale, w, w_scale, bias=None, relu: bool = False) -> None:
@@ -505,7 +512,7 @@ def _check_adamw(status: int, opt: Optional[_AdamW]) -> None:
 
 
 def _dtype_name(t, what: str) -> str:
-    name = str(t.dtype).removeprefix("torch.")
+    name = _NAME_OF.get(t.dtype) or _name_of(t.dtype)
     if name not in _TYPE_OF:
         raise TypeError(f"{what}: need float32, bfloat16 or float16, got {t.dtype}")
     return name
@@ -517,7 +524,7 @@ def _pointers(tensors, sizes, names, what: str):
         return None
     if len(tensors) != len(sizes):
         raise ValueError(f"{what}: {len(tensors)} tensors, need {len(sizes)}")
-    return (ctypes.c_void_p * len(sizes))(*[_ptr(t, name, n, what) for t, n, name in zip(tensors, sizes, names)])
+    return (ctypes.c_void_p * len(sizes))(*map(_ptr, tensors, names, sizes, itertools.repeat(what)))
 
 
 def st_adamw_create(params, exp_avg, exp_avg_sq, grads=None, exp_avg_scale=None, exp_avg_sq_scale=None, masters=None, *,
@@ -581,13 +588,13 @@ def st_adamw_step(opt: _AdamW, grad_scale: float = 1.0, norm_out=None) -> None:
 
 def st_adamw_read_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
     """The moments as float32 values into lists of CUDA tensors (an entry or a list may be None)."""
-    names = ["float32"] * len(opt.sizes)
+    names = itertools.repeat("float32")
     _check_adamw(load_library().st_adamw_read_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
                                                       _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
 
 
 def st_adamw_write_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
-    names = ["float32"] * len(opt.sizes)
+    names = itertools.repeat("float32")
     _check_adamw(load_library().st_adamw_write_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
                                                        _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
 
