@@ -40,19 +40,20 @@ struct TensorRec {              // does not change as long as the optimiser live
     uint8_t param_type, grad_type, vec, pad;                // vec: all buffers but the gradient lie as the vector path needs them
 };
 struct ChunkRec { int32_t tensor, index; };
-struct Scalars {
+struct __align__(32) Scalars {
     long long t;                // steps taken
-    double lr;
     float bias[2][2];           // of step t at [t % 2]: 1 / (1 - beta1^t) and 1 / sqrt(1 - beta2^t)
+    float lr;
     float factor;               // of the gradients, from the norm
     int skip;                   // the norm is not finite and the step is to be left out
     unsigned int norm_ticket, step_ticket;
+    double power[2];            // beta1^t and beta2^t of the next step
 };
 struct Plan {
     const TensorRec* tensors; const ChunkRec* chunks; int64_t n_chunks;
     const void** grads;
     Scalars* sc; double* partials;
-    double ln_b1, ln_b2, max_norm;
+    double beta1, beta2, max_norm;
     float b1, b2, omb1, omb2, eps, one;
     int skip_nonfinite;
 };
@@ -498,13 +499,14 @@ __device__ __noinline__ void step_block_slow(const TensorRec* t, const void* gra
     step_block<BITS, false>(*t, t->param_type, t->grad_type, t->master != nullptr, grad, k, at, (int)min(t->n - at, (int64_t)kBlockVals), lane);
 }
 
-__device__ __forceinline__ void bias_corrections(const Plan& p, long long t, float (&out)[2])
+__host__ __device__ inline void bias_corrections(const double (&power)[2], float (&out)[2])
 {
-    out[0] = (float)(-1.0 / expm1((double)t * p.ln_b1));
-    out[1] = (float)(1.0 / sqrt(-expm1((double)t * p.ln_b2)));
+    out[0] = (float)(1.0 / (1.0 - power[0]));
+    out[1] = (float)(1.0 / sqrt(1.0 - power[1]));
 }
 
-// Block 0 works the next step's bias corrections out (two exponentials in double, over a microsecond); the others step the tensors.
+// Block 0 works the next step's bias corrections out; the others step the tensors.  (As exponentials they took over a microsecond; a product
+// per step is off by 1e-16 of itself a step, when the power has long ceased to matter.)
 template <int BITS>
 __global__ void __launch_bounds__(kThreads, BITS == 32 ? 4 : 5) adamw_step_kernel(const __grid_constant__ Plan p, float grad_scale, int with_norm)
 {
@@ -512,12 +514,20 @@ __global__ void __launch_bounds__(kThreads, BITS == 32 ? 4 : 5) adamw_step_kerne
     if (blockIdx.x) share = share_of(p, 0, p.n_chunks, blockIdx.x - 1, gridDim.x - 1);
     pdl_wait();
     pdl_launch_dependents();
-    const long long t = p.sc->t + 1;                    // every thread reads it: the step that is taken
-    const bool skip = with_norm && p.sc->skip;
+    Scalars* const sc = p.sc;
+    const long long t = sc->t + 1;                      // every thread reads it: the step that is taken
+    const float bias[2][2] = {{sc->bias[0][0], sc->bias[0][1]}, {sc->bias[1][0], sc->bias[1][1]}}, lr = sc->lr, factor = sc->factor;   // all on their way together
+    const bool skip = with_norm && sc->skip;
     if (blockIdx.x == 0) {
-        if (threadIdx.x == 0 && !skip) bias_corrections(p, t + 1, p.sc->bias[(t + 1) & 1]);
+        if (threadIdx.x == 0 && !skip) {
+            const double power[2] = {sc->power[0] * p.beta1, sc->power[1] * p.beta2};
+            float next[2];
+            bias_corrections(power, next);
+            sc->power[0] = power[0]; sc->power[1] = power[1];
+            sc->bias[(t + 1) & 1][0] = next[0]; sc->bias[(t + 1) & 1][1] = next[1];
+        }
     } else if (!skip) {
-        const StepNow k = {p.sc->bias[t & 1][0], p.sc->bias[t & 1][1], (float)p.sc->lr, with_norm ? p.sc->factor : grad_scale,
+        const StepNow k = {t & 1 ? bias[1][0] : bias[0][0], t & 1 ? bias[1][1] : bias[0][1], lr, with_norm ? factor : grad_scale,
                            p.b1, p.b2, p.omb1, p.omb2, p.eps, p.one};
         const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
         walk(p, share, [&](int i, const TensorRec& t, int64_t begin, int64_t end) {
@@ -530,14 +540,12 @@ __global__ void __launch_bounds__(kThreads, BITS == 32 ? 4 : 5) adamw_step_kerne
             for (; at < end; at += kChunk) step_block_slow<BITS>(p.tensors + i, grad, k, at, lane);
         });
     }
-    // the block that finishes last counts the step: every block has read the count by then
+    // The block that finishes last counts the step: every thread of every block has read the count by then.  (No fence: nothing that the
+    // blocks have written is read before the kernel is complete.)
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(&p.sc->step_ticket, 1u) == gridDim.x - 1) {
-            p.sc->step_ticket = 0;
-            if (!skip) p.sc->t = t;
-        }
+    if (threadIdx.x == 0 && atomicAdd(&sc->step_ticket, 1u) == gridDim.x - 1) {
+        sc->step_ticket = 0;
+        if (!skip) sc->t = t;
     }
 }
 
@@ -618,7 +626,7 @@ __global__ void adamw_set_grads_kernel(const void** grads, int first, int count,
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     if (i < count) grads[first + i] = a.q[i];
 }
-__global__ void adamw_set_lr_kernel(Scalars* sc, double lr) { sc->lr = lr; }
+__global__ void adamw_set_lr_kernel(Scalars* sc, float lr) { sc->lr = lr; }
 
 // ---- moments as fp32 values and back -----------------------------------------------------------------------
 // Tensors [first, ...) of chunks [chunk_begin, chunk_end) with their pointers in the arguments: m's at 2 i, v's at 2 i + 1
@@ -875,15 +883,14 @@ st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adam
     p.sc = (Scalars*)b; p.partials = (double*)(b + at_partials); p.tensors = (const TensorRec*)(b + at_tensors); p.grads = (const void**)(b + at_grads);
     p.chunks = (const ChunkRec*)(b + at_chunks);
     p.n_chunks = n_chunks;
-    p.ln_b1 = log(d.beta1); p.ln_b2 = log(d.beta2); p.max_norm = d.max_norm;
+    p.beta1 = d.beta1; p.beta2 = d.beta2; p.max_norm = d.max_norm;
     p.b1 = (float)d.beta1; p.b2 = (float)d.beta2; p.omb1 = (float)(1.0 - d.beta1); p.omb2 = (float)(1.0 - d.beta2); p.eps = (float)d.eps; p.one = 1.f;
     p.skip_nonfinite = d.skip_nonfinite;
     o->always_norm = d.max_norm > 0 || d.skip_nonfinite;
     Scalars sc = {};
-    sc.t = d.first_step; sc.lr = d.lr; sc.factor = 1.f;
-    const double next = (double)d.first_step + 1;
-    sc.bias[(d.first_step + 1) & 1][0] = (float)(-1.0 / expm1(next * p.ln_b1));
-    sc.bias[(d.first_step + 1) & 1][1] = (float)(1.0 / sqrt(-expm1(next * p.ln_b2)));
+    sc.t = d.first_step; sc.lr = (float)d.lr; sc.factor = 1.f;
+    sc.power[0] = pow(d.beta1, (double)d.first_step + 1); sc.power[1] = pow(d.beta2, (double)d.first_step + 1);
+    bias_corrections(sc.power, sc.bias[(d.first_step + 1) & 1]);
     std::vector<const void*> grads(d.n_tensors);
     for (int i = 0; i < d.n_tensors; ++i) grads[i] = tensors[i].n ? tensors[i].grad : nullptr;
     const struct { void* to; const void* from; size_t bytes; } copies[] = {
@@ -933,7 +940,7 @@ st_status st_adamw_create(const st_adamw_desc* desc, const st_adamw_tensor* tens
     const st_adamw_desc& d = *desc;
     if (d.n_tensors < 1 || d.n_tensors > 65535) return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: n_tensors %d outside 1..65535", d.n_tensors);
     if (d.state_bits != 32 && d.state_bits != 8) return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: state_bits must be 32 or 8");
-    if (!(d.lr >= 0) || !std::isfinite(d.lr) || !(d.beta1 >= 0 && d.beta1 < 1) || !(d.beta2 >= 0 && d.beta2 < 1) || !(d.eps >= FLT_MIN && d.eps <= FLT_MAX))
+    if (!(d.lr >= 0 && d.lr <= FLT_MAX) || !(d.beta1 >= 0 && d.beta1 < 1) || !(d.beta2 >= 0 && d.beta2 < 1) || !(d.eps >= FLT_MIN && d.eps <= FLT_MAX))
         return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: needs lr >= 0, beta1 and beta2 in [0, 1) and eps >= %g", (double)FLT_MIN);
     if (!(d.max_norm >= 0) || !std::isfinite(d.max_norm) || d.first_step < 0 || (d.skip_nonfinite & ~1))
         return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: needs max_norm >= 0, first_step >= 0 and skip_nonfinite 0 or 1");
@@ -966,10 +973,10 @@ st_status st_adamw_set_grads(st_adamw* o, const void* const* grads)
 st_status st_adamw_set_lr(st_adamw* o, double lr)
 {
     if (!o) return ST_ERR_INVALID_ARG;
-    if (!(lr >= 0) || !std::isfinite(lr)) return fail(o, ST_ERR_INVALID_ARG, "st_adamw_set_lr: lr must be >= 0");
+    if (!(lr >= 0 && lr <= FLT_MAX)) return fail(o, ST_ERR_INVALID_ARG, "st_adamw_set_lr: lr must be >= 0 and finite in fp32");
     OnDevice guard(o->device);
     if (!guard.ok) return fail(o, ST_ERR_CUDA, "st_adamw_set_lr: cannot use the optimiser's device");
-    adamw_set_lr_kernel<<<1, 1, 0, o->stream>>>(o->plan.sc, lr);
+    adamw_set_lr_kernel<<<1, 1, 0, o->stream>>>(o->plan.sc, (float)lr);
     return check_launch(o, "st_adamw_set_lr");
 }
 

@@ -4,10 +4,10 @@
 //
 // Both operands are K-major, so TMA's 128-byte-swizzled tiles go into tcgen05.mma kind::i8 (K = 32 bytes an instruction) as they
 // are; extents that are no multiples of a tile are TMA's zero fill.  Three forms:
-//   int8_tiles_kernel   many tokens: tokens are the accumulator's lanes, up to 256 channels its columns; a persistent block per SM, ring of
-//                       128-byte slices of K, two accumulators so that one is scaled and stored while the other is summed.
-//   int8_split_kernel   few tokens, or too few tiles for the SMs: channels are the lanes, up to 128 tokens the columns; the blocks of a
-//                       cluster share a tile's K range and add their sums through distributed shared memory.
+//   int8_tiles_kernel   more tokens: tokens are the accumulator's lanes, 64, 128 or 256 channels its columns; a persistent block per SM, ring of
+//                       128-byte slices of K, two or four accumulators so that some are scaled and stored while the next is summed.
+//   int8_split_kernel   up to 128 tokens: channels are the lanes, tokens the columns; the blocks of a cluster share a tile's K range and add
+//                       their sums through distributed shared memory.
 //   int8_plain_kernel   operands that TMA cannot read (bases or pitches that are no multiples of 16 bytes): dp4a.
 #include "../../include/shadowtutor.h"
 #include "st_internal.h"
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     if (warp == 2) tmem_dealloc(tmem, Shape::cols);
 }
 
-// ---- few tokens, or few tiles --------------------------------------------------------------------------------------
+// ---- few tokens --------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 192;              // four warps that store, producer, issuer
 constexpr int kMaxSplitStages = 8, kMaxSplits = 8;
 struct SplitArgs { Out out; int slices, splits, stages; unsigned int* err; uint32_t stall; };
@@ -358,13 +358,13 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    const int split = blockIdx.x % a.splits, n0 = blockIdx.x / a.splits * kTile, m0 = blockIdx.y * BT;
+    const int split = blockIdx.x % a.splits, n0 = blockIdx.x / a.splits * kTile;
     const int begin = (int)((int64_t)a.slices * split / a.splits), end = (int)((int64_t)a.slices * (split + 1) / a.splits);
     const Out& o = a.out;
     pdl_wait();
     pdl_launch_dependents();
     bool ok = true;
-    const int count = min(o.M - m0, BT);        // tokens of the tile
+    const int count = o.M;                      // tokens, at most BT
     if (warp == 4) {
         if (elect_one()) {
             uint32_t stage = 0, phase = 1;
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
                 const uint32_t bar = smem_u32(&full[stage]), dst = ring + stage * kStage;
                 mbar_expect_tx(bar, kStage + (s == begin ? a.stall : 0u));
                 tma_load_2d(dst, &tm_w, bar, s * kSlice, n0);
-                tma_load_2d(dst + kTile * kSlice, &tm_x, bar, s * kSlice, m0);
+                tma_load_2d(dst + kTile * kSlice, &tm_x, bar, s * kSlice, 0);
                 if (++stage == (uint32_t)a.stages) { stage = 0; phase ^= 1; }
             }
         }
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
                 if (a.splits == 1) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (mine && c0 + j < count) put_one(o, (int64_t)(m0 + c0 + j) * o.ldy + channel, finish(__float_as_int(v[j]), o.sx[m0 + c0 + j], sw, bias, o.least));
+                        if (mine && c0 + j < count) put_one(o, (int64_t)(c0 + j) * o.ldy + channel, finish(__float_as_int(v[j]), o.sx[c0 + j], sw, bias, o.least));
                 } else {                        // every MMA has read its operands: the ring is free
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kSplitThreads) int8_split_kernel(const __grid_
                 int4 sum = part[0];
 #pragma unroll
                 for (int r = 1; r < kMaxSplits; ++r) { sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w; }
-                put_four(o, m0 + c, channel, sum, o.sx[m0 + c], sw, bias);
+                put_four(o, c, channel, sum, o.sx[c], sw, bias);
             }
         }
         __syncwarp();
@@ -567,13 +567,24 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     char msg[160] = "";
     CUtensorMap tx, tw;
     const int slices = (int)((p.K + kSlice - 1) / kSlice);
-    const char* form = getenv("ST_INT8_FORM");
-    if (form ? form[0] == 's' : p.M <= 128) {
-        const int bt = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
-        const int64_t m_tiles = (p.M + bt - 1) / bt, n_tiles = (p.N + kTile - 1) / kTile;
-        int splits = 1;
-        while (splits < 8 && m_tiles * n_tiles * splits * 2 <= d->sms + 20 && slices >= splits * 2) splits *= 2;
-        if (form && form[1]) splits = std::min(form[1] - '0', slices >= 8 ? 8 : slices >= 4 ? 4 : slices >= 2 ? 2 : 1);
+    // What the forms would take, in microseconds: launch and ends, then for each round of tiles the slices and what storing adds, fitted to 36 shapes
+    // from 1 x 256 x 256 to 57600 x 512 x 256 that both were run on (off by 20 per cent at most; 16 x 4096 x 4096: 6.3 measured for clusters, 9.7 for
+    // tiles of 64 columns; 128 x 4096 x 4096: 12 and 10; 4096 x 1024 x 1024: 11.4, 8.7 and 7.5 for tiles of 64, 128 and 256 columns).
+    const auto tiles_time = [&](int columns) {
+        const double slice = columns == 64 ? 0.20 : columns == 128 ? 0.22 : 0.33, store = columns / 160.0;
+        const int64_t tiles = (p.M + kTile - 1) / kTile * ((p.N + columns - 1) / columns), rounds = (tiles + d->sms - 1) / d->sms;
+        return 3.3 + (double)rounds * (slices * slice + store);
+    };
+    int bn = 64;
+    for (int columns : {128, 256})
+        if (tiles_time(columns) < tiles_time(bn)) bn = columns;
+    const int bt = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    const int64_t n_split_tiles = (p.N + kTile - 1) / kTile;
+    // As many blocks to a tile as the SMs allow (a few more blocks than SMs are let in: two of them fit one), with two slices of K each at least
+    int splits = 1;
+    while (splits < kMaxSplits && n_split_tiles * splits * 2 <= d->sms + 20 && slices >= splits * 2) splits *= 2;
+    const double weight_time = (double)p.N * (double)p.K / 5.5e6, slice_time = 0.16 * ((slices + splits - 1) / splits) * (double)((n_split_tiles * splits + d->sms - 1) / d->sms);
+    if (p.M <= 128 && 2.6 + std::max(weight_time, slice_time) + 0.04 * bt < tiles_time(bn)) {
         SplitArgs a;
         a.out = o; a.slices = slices; a.splits = splits; a.err = d->err_dev; a.stall = stall_bytes();
         const int stage = (kTile + bt) * kSlice, per = (slices + splits - 1) / splits;
@@ -582,7 +593,7 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
         if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, bt, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, kTile, msg, sizeof msg, "w"))
             return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(n_tiles * splits), (unsigned)m_tiles); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = bytes; cfg.stream = s;
+        cfg.gridDim = dim3((unsigned)(n_split_tiles * splits)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = bytes; cfg.stream = s;
         cudaLaunchAttribute at[2];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim.x = (unsigned)splits; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
@@ -593,7 +604,6 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
           : bt == 64 ? cudaLaunchKernelEx(&cfg, int8_split_kernel<64>, tx, tw, a) : cudaLaunchKernelEx(&cfg, int8_split_kernel<128>, tx, tw, a);
         return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
     }
-    const int bn = getenv("ST_INT8_BN") ? atoi(getenv("ST_INT8_BN")) : p.N <= 64 ? 64 : p.N <= 128 ? 128 : 256;
     TilesArgs a;
     a.out = o; a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
     // Rows of a tile: 128, or fewer where as many rounds of tiles then fill all SMs evenly.  (57600 x 512 x 256: 450 tiles of 128 rows are 3.04
@@ -650,7 +660,7 @@ extern "C" st_status st_int8_matmul(const int8_t* x, int64_t ldx, const float* x
     if (ldx < K || ldw < K || ldy < N) return bad("ldx, ldw below K or ldy below N");
     if (K > kMaxInt8K) return (st_status)fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: K above %d could overflow the 32-bit sums", kMaxInt8K);
     if (M > kMaxInt8Extent - 255 || N > kMaxInt8N || !extent_fits(M, ldx, K, 1) || !extent_fits(N, ldw, K, 1) || !extent_fits(M, ldy, N, 1) ||
-        ((M + 127) / 128) * ((N + 63) / 64) > kMaxInt8Extent)
+        ((M + 127) / 128) * ((N + 63) / 64) > kMaxInt8Extent / 2)
         return (st_status)fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: extents beyond the kernels' 32-bit counts of tiles");
     if (M == 0 || N == 0) return ST_OK;
     Int8Buffers b("st_int8_matmul");

@@ -174,6 +174,15 @@ def test_products(m, n, k):
     check_matmul(m, n, k, "f32", bias=False, relu=True, seed=n)
 
 
+# shapes that each width of tile, with and without weights that stay, one round and several, two and four groups that store, and each token count of
+# the cluster form is taken for
+@pytest.mark.parametrize("m,n,k", [(30, 4096, 2048), (60, 4100, 4096), (100, 1000, 300), (16, 130, 8192), (3, 20000, 256), (9000, 64, 700), (20011, 384, 384),
+                                   (4100, 1024, 1024), (30000, 256, 512), (30001, 250, 1024), (4099, 4096, 512), (3001, 5000, 2500), (2048, 2304, 3000)])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_products_of_every_form(m, n, k, kind):
+    check_matmul(m, n, k, kind, relu=True, seed=k)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 33, 70), (50, 257, 300), (333, 100, 64), (5000, 300, 200)])
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
 def test_products_of_any_layout(m, n, k, kind):
