@@ -325,6 +325,33 @@ def test_moments_go_out_and_come_back(bits):
     assert all(torch.equal(a, b) for a, b in zip(before[0], other[4])) and torch.equal(before[1], other[3][2])
 
 
+def test_values_at_the_ends_of_the_range_step_like_others():
+    """Moments that are 0, subnormal or near fp32's end, in one warp with ordinary ones."""
+    vals = np.array([0.0, 1e-45, 1e-40, 1.2e-38, 1e-37, 1e-31, 1e-30, 1e-20, 1e-8, 1.0, 1e10, 1e30, 3e38])
+    m0, v0 = [x.reshape(-1) for x in np.meshgrid(np.concatenate([-vals, vals]), vals)]
+    n = m0.size
+    for g0 in (0.0, 1e-3):
+        made = make([n], 32, wd=0.0, eps=1e-12, lr=1e-3)
+        opt, params, _, m, v, _, grads, refs = made
+        st.st_adamw_write_moments(opt, [put(m0, "f32")], [put(v0, "f32")])
+        grads[0].fill_(g0)
+        r = refs[0]
+        r.m, r.v = f64(m[0]), f64(v[0])
+        before = f64(params[0])
+        st.st_adamw_step(opt)
+        r.step(f64(grads[0]))
+        tiny = 2.0 ** -149
+        assert np.all(np.abs(f64(m[0]) - r.m) <= 5 * U * np.abs(r.m) + 5 * U * g0 + tiny)
+        assert np.all(np.abs(f64(v[0]) - r.v) <= 8 * U * r.v + tiny)
+        # v of a few subnormal steps has that much relative error, and its root half of it
+        rough = 0.5 * tiny / np.maximum(r.v, tiny)
+        step = before - r.p
+        off = r.bound + rough * np.abs(step) + 4 * U * np.abs(step)
+        # quotients m / (sqrt(v) + eps) that fp32 holds: beyond FLT_MAX they are infinite, and so is the step
+        ok = np.abs(step) * (1 - 0.9) / 1e-3 < 3.4e38
+        assert np.all(np.abs(f64(params[0]) - r.p)[ok] <= off[ok] + tiny)
+
+
 def test_negative_second_moments_are_taken_as_zero():
     for bits in (32, 8):
         made = make([10], bits)
