@@ -181,10 +181,10 @@ __device__ __forceinline__ void decode(float (&m)[kPer], float (&root)[kPer], co
     }
 }
 
-// The level floor(sqrt(r) + 1/2).  The approximate root lies within 2^-23 of the root (relative; 3e-5 of a level at level 255,
-// and as much again where `r` comes from an approximate root), so rounding it to the nearest whole number gives the level unless it lies as near as kNear to a border; there the border, which fp32 holds
-// exactly, decides.  One in 5000 values does: a lane that has met one among its sixteen takes that path for all of them.
-constexpr float kNear = 1e-4f, kRound = 12582912.f;         // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
+// The level floor(sqrt(r) + 1/2).  The approximate root lies within 2^-23 of the root, and so does that of a ratio formed from an approximate root
+// (half of 2^-23 and 2^-24 more).  So rounding it to the nearest whole number gives the level unless it lies next to a border: within
+// 127 * 2^-23 = 1.6e-5 of one for m, 255 * 1.75 * 2^-23 = 5.4e-5 for sqrt(v).  There the border, which fp32 holds exactly, decides.
+constexpr float kNearM = 2e-5f, kNearV = 6e-5f, kRound = 12582912.f;        // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
 __device__ __forceinline__ float approximate_root(float r)
 {
     float s;
@@ -213,17 +213,18 @@ __device__ __forceinline__ void encode(const float (&m)[kPer], const float (&roo
     m_scale = a < 0x1p-100f ? 0.f : __fdiv_rn(a, 127.f * 127.f);
     v_scale = __fdiv_rn(b, 255.f * 255.f);
     const float im = m_scale > 0.f ? __frcp_rn(m_scale) : 0.f, iv = v_scale > 0.f ? __frcp_rn(v_scale) : 0.f;
-    float far = 0.f;
+    float far_m = 0.f, far_v = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const float s = copysignf(approximate_root(__fmul_rn(fabsf(m[j]), im)), m[j]), y = s + kRound;
         // a second moment that is not 0 has level 1 at least (the least root is 3.7e-23)
         const float r = fmaxf(approximate_root(__fmul_rn(root[j], iv)), __saturatef(root[j] * FLT_MAX)), z = r + kRound;
-        far = fmaxf(far, fmaxf(fabsf(s - (y - kRound)), fabsf(r - (z - kRound))));
+        far_m = fmaxf(far_m, fabsf(s - (y - kRound)));
+        far_v = fmaxf(far_v, fabsf(r - (z - kRound)));
         cm[j] = __float_as_uint(y);
         cv[j] = __float_as_uint(z);
     }
-    if (far > 0.5f - kNear) {
+    if (far_m > 0.5f - kNearM || far_v > 0.5f - kNearV) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const float c = exact_level(__fmul_rn(fabsf(m[j]), im)), d = exact_level(__fmul_rn(root[j], iv));
@@ -376,7 +377,7 @@ __device__ __forceinline__ void fetch_8(Loads8& l, const TensorRec& t, const voi
     else fetch<true>(l.p, t.param, PARAM, at, kBlockVals, lane);
 }
 // A lane's codes of a block, exactly, from what the block's step reads (old codes and scales, which must not have been overwritten) and the
-// reciprocals of its new scales.  Out of line: a lane in 300 comes here, and its registers are not the step's.
+// reciprocals of its new scales.  Out of line: a lane in 800 comes here, and its registers are not the step's.
 template <int GRAD>
 __device__ __noinline__ uint4 exact_codes(const TensorRec* t, const void* grad, StepNow k, int64_t at, float im, float iv)
 {
@@ -449,7 +450,7 @@ __device__ __forceinline__ void step_block_8(const TensorRec* record, const Tens
         if (MASTER) put<true>(x, t.master, ST_F32, at, kBlockVals, lane);
     }
     uint32_t cm[kPer], cv[kPer];
-    float far = 0.f;
+    float far_m = 0.f, far_v = 0.f;
     const f32x2 im2 = both(im), iv2 = both(iv), up = both(kRound), down = both(-kRound), minus = both(-1.f);
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) {
@@ -460,14 +461,14 @@ __device__ __forceinline__ void step_block_8(const TensorRec* record, const Tens
         const f32x2 r = pack2(fmaxf(approximate_root(r0), __saturatef(root[2 * q] * FLT_MAX)), fmaxf(approximate_root(r1), __saturatef(root[2 * q + 1] * FLT_MAX)));
         const f32x2 y = add2(s, up), z = add2(r, up);
         unpack2(fma2(add2(y, down), minus, s), e0, e1);
-        far = fmaxf(far, fmaxf(fabsf(e0), fabsf(e1)));
+        far_m = fmaxf(far_m, fmaxf(fabsf(e0), fabsf(e1)));
         unpack2(fma2(add2(z, down), minus, r), e0, e1);
-        far = fmaxf(far, fmaxf(fabsf(e0), fabsf(e1)));
+        far_v = fmaxf(far_v, fmaxf(fabsf(e0), fabsf(e1)));
         cm[2 * q] = (uint32_t)y; cm[2 * q + 1] = (uint32_t)(y >> 32);
         cv[2 * q] = (uint32_t)z; cv[2 * q + 1] = (uint32_t)(z >> 32);
     }
     uint4 codes = make_uint4(low_bytes(cm), low_bytes(cm + 4), low_bytes(cv), low_bytes(cv + 4));
-    if (far > 0.5f - kNear) codes = exact_codes<GRAD>(record, grad, k, at, im, iv);
+    if (far_m > 0.5f - kNearM || far_v > 0.5f - kNearV) codes = exact_codes<GRAD>(record, grad, k, at, im, iv);
     __syncwarp();                                               // nobody reads the old scales any more
     *(uint2*)((uint8_t*)t.m + at + kPer * lane) = make_uint2(codes.x, codes.y);
     *(uint2*)((uint8_t*)t.v + at + kPer * lane) = make_uint2(codes.z, codes.w);
