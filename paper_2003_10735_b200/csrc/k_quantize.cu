@@ -124,11 +124,11 @@ __device__ __forceinline__ float beside_half(float x, float t, float scale)
     const float h = k + copysignf(0.5f, d), over = fmaf(-h, scale, x);
     return over > 0.f ? h + 0.5f : over < 0.f ? h - 0.5f : rintf(h);
 }
-// The integers of V values (4 or 8) that lie at `at`, packed in words
-template <typename T, int V>
-__device__ __forceinline__ void quantize(uint32_t (&w)[V / 4], const float (&x)[V], const T* at, int64_t stride, int n, const RowScale& r)
+// The integers of V values (4 or 8), packed in words
+template <int V>
+__device__ __forceinline__ void quantize(uint32_t (&w)[V / 4], const float (&x)[V], const RowScale& r)
 {
-    float far = r.doubt;
+    float far = 0.f;
     uint32_t b[V];
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
@@ -141,14 +141,11 @@ __device__ __forceinline__ void quantize(uint32_t (&w)[V / 4], const float (&x)[
         b[j] = (uint32_t)y;
         b[j + 1] = (uint32_t)(y >> 32);
     }
-    if (far > 0.5f - kNear && r.doubt == 0.f)
+    if (far > 0.5f - kNear)
 #pragma unroll
         for (int j = 0; j < V; ++j) b[j] = __float_as_uint(beside_half(x[j], x[j] * r.inverse, r.scale) + kRound);
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) w[i] = low_bytes(b + 4 * i) & r.mask;
-    if (r.doubt != 0.f)
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i) w[i] = exact_integers(at + 4 * i * stride, stride, min(n - 4 * i, 4), r.scale);
 }
 template <typename T>
 __device__ __forceinline__ uint8_t quantize_one(const T* at, const RowScale& r)
@@ -174,12 +171,14 @@ __device__ __forceinline__ RowParts parts_of(const T* row, int cols)
 // W warps to a row.  ALIGNED: rows of x and q begin where whole pieces can be read and written, and cols is a multiple of V.  Otherwise the integers
 // of a row are gathered in shared memory and written from there in aligned words, whatever the alignment of x's and q's rows.
 // KEEP: a row fits kItems pieces per lane; otherwise it is read twice, the second time in stretches of that many.
-constexpr int kItems = 8;
+// Pieces a lane keeps, and blocks an SM should hold.  Where pieces go straight to q, many small blocks are best (8192 x 4096 bf16: 21.0 us with four
+// pieces and six blocks, 24.8 with eight and three); rows that go through shared memory want fewer warps to wait for (4099 x 1111: 9.0 with eight, 13).
+constexpr int kItemsStraight = 4, kItemsGathered = 8;
 template <typename T, int W, bool ALIGNED, bool KEEP>
-__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride,
+__global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 2) quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride,
                                                                  int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale)
 {
-    constexpr int V = Piece<T>::V, kLanes = 32 * W, kRows = kThreads / kLanes, kStretch = kItems * kLanes;     // pieces
+    constexpr int V = Piece<T>::V, kLanes = 32 * W, kItems = ALIGNED ? kItemsStraight : kItemsGathered, kRows = kThreads / kLanes, kStretch = kItems * kLanes;     // pieces
     constexpr int kPitch = kStretch * V + 32;               // bytes of a row's stretch with its head and tail, and what aligning it takes
     __shared__ uint32_t tops[kThreads / 32];
     __shared__ __align__(16) uint8_t gathered[ALIGNED ? 16 : kRows * kPitch];
@@ -224,16 +223,16 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __rest
     }
     const RowScale r = row_scale(bits);
     if (mine && me == 0) scale[row] = r.scale;
-    const auto pack = [&](uint32_t (&w)[V / 4], const Piece<T>& k, int i) {
+    const auto pack = [&](uint32_t (&w)[V / 4], const Piece<T>& k) {
         float v[V];
         k.get(v);
-        quantize<T, V>(w, v, src + p.head + i * V, 1, V, r);
+        quantize<V>(w, v, r);
     };
     if (ALIGNED) {
         if (!mine) return;
         const auto put = [&](const Piece<T>& k, int i) {
             uint32_t w[V / 4];
-            pack(w, k, i);
+            pack(w, k);
             if constexpr (V == 8) *(uint2*)(dst + i * V) = make_uint2(w[0], w[1]);
             else *(uint32_t*)(dst + i * V) = w[0];
         };
@@ -245,6 +244,9 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __rest
 #pragma unroll 4
             for (int i = me; i < p.pieces; i += kLanes) { get(kept[0], i); put(kept[0], i); }
         }
+        if (r.doubt != 0.f)                     // the row once more, the same lanes at the same places
+            for (int i = me; i < p.pieces; i += kLanes)
+                for (int j = 0; j < V; j += 4) *(uint32_t*)(dst + i * V + j) = exact_integers(src + i * V + j, 1, 4, r.scale);
         return;
     }
     // integer c of the row lies at buf[c - first]; buf is placed so that pieces lie at multiples of 8
@@ -262,11 +264,14 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __rest
                 if (at >= p.pieces) continue;
                 if (!KEEP) get(kept[i], at);
                 uint32_t w[V / 4];
-                pack(w, kept[i], at);
+                pack(w, kept[i]);
                 uint8_t* to = buf + p.head + at * V - first;
                 if constexpr (V == 8) *(uint2*)to = make_uint2(w[0], w[1]);
                 else *(uint32_t*)to = w[0];
             }
+            if (r.doubt != 0.f)                 // once more, the same lanes at the same places
+                for (int at = begin + me; at < min(begin + kStretch, p.pieces); at += kLanes)
+                    for (int j = 0; j < V; j += 4) *(uint32_t*)(buf + p.head + at * V + j - first) = exact_integers(src + p.head + at * V + j, 1, 4, r.scale);
         }
         if (W == 1) __syncwarp(); else __syncthreads();
         if (mine) {
@@ -354,8 +359,11 @@ __global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(co
                 if (c >= n) continue;
                 const float v[4] = {to_float(kept[i][0][u]), to_float(kept[i][1][u]), to_float(kept[i][2][u]), to_float(kept[i][3][u])};
                 uint32_t w[1];
-                quantize<T, 4>(w, v, (UNIT ? src[0] + 32 * u : src[UNIT ? 0 : u]) + (slab + c) * col_stride, col_stride, n - c, r);
+                quantize<4>(w, v, r);
                 *(uint32_t*)(turned + (32 * u + lane) * kSlabPitch + c) = w[0];
+                if (r.doubt != 0.f)
+                    *(uint32_t*)(turned + (32 * u + lane) * kSlabPitch + c) =
+                        exact_integers((UNIT ? src[0] + 32 * u : src[UNIT ? 0 : u]) + (slab + c) * col_stride, col_stride, min(n - c, 4), r.scale);
             }
         }
         __syncthreads();
@@ -405,7 +413,7 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
         return launch_early(early, kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kThreads), 0, s, x, rows, n, rs, q, ldq, scale);
     };
     // as few warps to a row as hold it in registers
-    const int64_t room = 32 * kItems * V;
+    const int64_t room = 32 * (whole ? kItemsStraight : kItemsGathered) * V;
     if (whole) {
         if (cols <= room) return go(quantize_rows_kernel<T, 1, true, true>, 1);
         if (cols <= 2 * room) return go(quantize_rows_kernel<T, 2, true, true>, 2);
