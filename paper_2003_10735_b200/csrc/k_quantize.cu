@@ -311,11 +311,13 @@ __global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(co
     T kept[kGroups][4][P];
     Top<T> top[P];
     const auto fetch = [&](T (&k)[4][P], int c) {
+        const int last = cols - 1 - c;
+        int64_t at = c * col_stride;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t at = min(c + j, cols - 1) * col_stride;
 #pragma unroll
             for (int u = 0; u < P; ++u) k[j][u] = UNIT ? src[0][at + 32 * u] : src[UNIT ? 0 : u][at];
+            at += j < last ? col_stride : 0;
         }
     };
     for (int slab = 0; slab < cols; slab += kSlab) {
