@@ -3,9 +3,10 @@
 // Sums are exact in 32-bit integers; the four fp32 operations behind them are rounded one by one, in the order above.
 //
 // Both operands are K-major, so TMA's 128-byte-swizzled tiles go into tcgen05.mma kind::i8 (K = 32 bytes an instruction) as they
-// are; extents that are no multiples of a tile are TMA's zero fill.  Three forms:
+// are; extents that are no multiples of a tile are TMA's zero fill.  Four forms:
 //   int8_tiles_kernel   more tokens: tokens are the accumulator's lanes, 64, 128 or 256 channels its columns; a persistent block per SM, ring of
 //                       128-byte slices of K, two or four accumulators so that some are scaled and stored while the next is summed.
+//   int8_pair_kernel    deep K: two SMs to a tile of 256 x 256.
 //   int8_split_kernel   up to 128 tokens: channels are the lanes, tokens the columns; the blocks of a cluster share a tile's K range and add
 //                       their sums through distributed shared memory.
 //   int8_plain_kernel   operands that TMA cannot read (bases or pitches that are no multiples of 16 bytes): dp4a.
@@ -52,6 +53,14 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
 }
 __device__ __forceinline__ int std_min(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank)
+{
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 struct Out {
     void* y; int64_t ldy; int type, wide;       // wide: rows of y take whole 16-byte stores
@@ -141,6 +150,93 @@ __device__ __forceinline__ void stage_and_store(const float (&v)[32], uint32_t p
     }
 }
 
+// What the groups of warps that store do.  `rank` of BLOCKS that share a tile: the tile's rows are split between them.  acc_full: this block's barriers;
+// acc_empty: those of the block that issues (cluster addresses where it may be another).  False: a wait gave up.
+template <int BN, int ACCS, int BLOCKS>
+__device__ __forceinline__ bool scale_and_store(const TilesArgs& a, const CUtensorMap& tm_y, const CUtensorMap& tm_y_rest, uint8_t* smem_raw, uint32_t staging, float* column,
+                                                uint32_t tmem, uint32_t acc_full, uint32_t acc_empty, int warp, int lane, int first, int step, int tiles, int rank)
+{
+    constexpr int kWidth = BN == 256 ? 128 : BN;            // columns of a group's share, of four groups; two have the room of four
+    bool ok = true;
+    const int group = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * group;
+    const int shares = std_min(a.groups / a.slots, BN / 32), width = BN / shares, slot = group / shares, c_begin = group % shares * width, c_most = c_begin + width;
+    const Out& o = a.out;
+    const bool whole_end = o.N * (o.type == ST_F32 ? 4 : 2) % 16 == 0;       // TMA leaves out the 16-byte pieces beyond y, but not the rest of one that y ends in
+    const uint32_t piece = staging + (warp - 4) * kPieceBytes;
+    float* const columns = column + group * 4 * (a.groups == 2 && BN == 256 ? 256 : kWidth);
+    int index = 0, turn = 0;
+    for (int t = first; t < tiles; t += step, ++index) {
+        if (index % a.slots != slot) continue;
+        const int acc = index % ACCS, acc_phase = index / ACCS & 1;
+        float *const scales = columns + turn * 2 * width - c_begin, *const biases = scales + width;       // of column c at [c]
+        turn ^= 1;
+        const int m0 = (t / a.n_tiles * BLOCKS + rank) * a.tile_m, n0 = t % a.n_tiles * BN;
+        const int64_t row = (int64_t)m0 + quarter * 32 + lane;
+        const bool mine = quarter * 32 + lane < a.tile_m && row < o.M;
+        const float sx = mine ? o.sx[row] : 0.f;
+        for (int c = c_begin + tid; c < c_most; c += 128) {
+            const bool in = n0 + c < o.N;
+            scales[c] = in ? o.sw[n0 + c] : 0.f;
+            biases[c] = in && o.bias ? o.bias[n0 + c] : 0.f;
+        }
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+        // a warp whose wait has given up goes on through the tiles without storing: the others wait for it above
+        if (ok) ok = mbar_wait(acc_full + 8 * acc, acc_phase, a.err, kWaitDone);
+        tc_fence_after_sync();
+        const int rows_in = min(min(a.tile_m, o.M - m0) - quarter * 32, 32);       // of this warp's 32
+        const CUtensorMap* tm_out = a.tile_m - quarter * 32 >= 32 ? &tm_y : &tm_y_rest;
+        const uint32_t lanes = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
+        const int c_end = ok && rows_in > 0 ? min(c_most, o.N - n0) : 0;
+#pragma unroll 1
+        for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+            float v[32];
+            __syncwarp();
+            tmem_ld_32x32(lanes + c0, v);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 sw = *(const float4*)(scales + c0 + j), b = *(const float4*)(biases + c0 + j);
+                finish2(v[j], v[j + 1], sx, sw.x, sw.y, b.x, b.y, o.least, o.one);
+                finish2(v[j + 2], v[j + 3], sx, sw.z, sw.w, b.z, b.w, o.least, o.one);
+            }
+            if (o.wide && (whole_end || n0 + c0 + 32 <= o.N)) {
+                // (57600 x 512 x 256: 27 us with lanes storing their own rows, 18.5 with the warp storing from shared memory, 17.3 in this way)
+                const int at_row = m0 + quarter * 32, at_col = n0 + c0;
+                if (o.type == ST_BF16) stage_and_store<ST_BF16>(v, piece, lane, tm_out, at_col, at_row, o.N);
+                else if (o.type == ST_F16) stage_and_store<ST_F16>(v, piece, lane, tm_out, at_col, at_row, o.N);
+                else stage_and_store<ST_F32>(v, piece, lane, tm_out, at_col, at_row, o.N);
+            } else {
+                // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
+                // 157 us with each lane storing its own row value by value, 30 in this way)
+                if (lane == 0) tma_store_wait_read<0>();
+                float* turned = (float*)(smem_raw + (piece - smem_u32(smem_raw)));
+                const int r0 = lane / 16, c = lane % 16;
+#pragma unroll
+                for (int h = 0; h < 32; h += 16) {
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) turned[lane * 16 + ((j + lane) & 15)] = v[h + j];
+                    __syncwarp();
+                    const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0 + h + c;
+                    if (n0 + c0 + h + c >= o.N) continue;
+                    if (o.type == ST_F32) {
+#pragma unroll 8
+                        for (int r = r0; r < rows_in; r += 2) ((float*)o.y)[first + r * o.ldy] = turned[r * 16 + ((c + r) & 15)];
+                    } else {
+#pragma unroll 8
+                        for (int r = r0; r < rows_in; r += 2) ((uint16_t*)o.y)[first + r * o.ldy] = round16(turned[r * 16 + ((c + r) & 15)], o.type);
+                    }
+                }
+            }
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) { if (BLOCKS == 1) mbar_arrive(acc_empty + 8 * acc); else mbar_arrive_cluster(acc_empty + 8 * acc); }
+    }
+    if (lane == 0) tma_store_wait();
+    __syncwarp();
+    return ok;
+}
+
 template <int BN>
 __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
 {
@@ -151,7 +247,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[Shape::accs], acc_empty[Shape::accs], w_full[kMaxResident];
     __shared__ uint32_t tmem_slot;
     // scales and bias of a tile's columns, for each group twice: a warp may be a tile ahead of the others of its group
-    constexpr int kWidth = BN == 256 ? 128 : BN;            // of four groups; two have the room of four
+    constexpr int kWidth = BN == 256 ? 128 : BN;
     __shared__ __align__(16) float column[kMaxGroups * 4 * kWidth];
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), Shape::cols);
@@ -223,83 +319,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
             }
         }
         __syncwarp();
-    } else if (warp >= 4) {                     // scale and store
-        const int group = (warp - 4) / 4, quarter = warp % 4, tid = threadIdx.x - 128 - 128 * group;
-        const int shares = std_min(a.groups / a.slots, BN / 32), width = BN / shares, slot = group / shares, c_begin = group % shares * width, c_most = c_begin + width;
-        const Out& o = a.out;
-        const bool whole_end = o.N * (o.type == ST_F32 ? 4 : 2) % 16 == 0;       // TMA leaves out the 16-byte pieces beyond y, but not the rest of one that y ends in
-        const uint32_t piece = staging + (warp - 4) * kPieceBytes;
-        float* const columns = column + group * 4 * (a.groups == 2 && BN == 256 ? 256 : kWidth);
-        int index = 0, turn = 0;
-        for (int t = (int)blockIdx.x; t < tiles; t += gridDim.x, ++index) {
-            if (index % a.slots != slot) continue;
-            const int acc = index % Shape::accs, acc_phase = index / Shape::accs & 1;
-            float *const scales = columns + turn * 2 * width - c_begin, *const biases = scales + width;       // of column c at [c]
-            turn ^= 1;
-            const int m0 = t / a.n_tiles * a.tile_m, n0 = t % a.n_tiles * BN;
-            const int64_t row = (int64_t)m0 + quarter * 32 + lane;
-            const bool mine = quarter * 32 + lane < a.tile_m && row < o.M;
-            const float sx = mine ? o.sx[row] : 0.f;
-            for (int c = c_begin + tid; c < c_most; c += 128) {
-                const bool in = n0 + c < o.N;
-                scales[c] = in ? o.sw[n0 + c] : 0.f;
-                biases[c] = in && o.bias ? o.bias[n0 + c] : 0.f;
-            }
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
-            // a warp whose wait has given up goes on through the tiles without storing: the others wait for it above
-            if (ok) ok = mbar_wait(smem_u32(&acc_full[acc]), acc_phase, a.err, kWaitDone);
-            tc_fence_after_sync();
-            const int rows_in = min(min(a.tile_m, o.M - m0) - quarter * 32, 32);       // of this warp's 32
-            const CUtensorMap* tm_out = a.tile_m - quarter * 32 >= 32 ? &tm_y : &tm_y_rest;
-            const uint32_t lanes = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
-            const int c_end = ok && rows_in > 0 ? min(c_most, o.N - n0) : 0;
-#pragma unroll 1
-            for (int c0 = c_begin; c0 < c_end; c0 += 32) {
-                float v[32];
-                __syncwarp();
-                tmem_ld_32x32(lanes + c0, v);
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    const float4 sw = *(const float4*)(scales + c0 + j), b = *(const float4*)(biases + c0 + j);
-                    finish2(v[j], v[j + 1], sx, sw.x, sw.y, b.x, b.y, o.least, o.one);
-                    finish2(v[j + 2], v[j + 3], sx, sw.z, sw.w, b.z, b.w, o.least, o.one);
-                }
-                if (o.wide && (whole_end || n0 + c0 + 32 <= o.N)) {
-                    // (57600 x 512 x 256: 27 us with lanes storing their own rows, 18.5 with the warp storing from shared memory, 17.3 in this way)
-                    const int at_row = m0 + quarter * 32, at_col = n0 + c0;
-                    if (o.type == ST_BF16) stage_and_store<ST_BF16>(v, piece, lane, tm_out, at_col, at_row, o.N);
-                    else if (o.type == ST_F16) stage_and_store<ST_F16>(v, piece, lane, tm_out, at_col, at_row, o.N);
-                    else stage_and_store<ST_F32>(v, piece, lane, tm_out, at_col, at_row, o.N);
-                } else {
-                    // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
-                    // 157 us with each lane storing its own row value by value, 30 in this way)
-                    if (lane == 0) tma_store_wait_read<0>();
-                    float* turned = (float*)(smem_raw + (piece - smem_u32(smem_raw)));
-                    const int r0 = lane / 16, c = lane % 16;
-#pragma unroll
-                    for (int h = 0; h < 32; h += 16) {
-                        __syncwarp();
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) turned[lane * 16 + ((j + lane) & 15)] = v[h + j];
-                        __syncwarp();
-                        const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0 + h + c;
-                        if (n0 + c0 + h + c >= o.N) continue;
-                        if (o.type == ST_F32) {
-#pragma unroll 8
-                            for (int r = r0; r < rows_in; r += 2) ((float*)o.y)[first + r * o.ldy] = turned[r * 16 + ((c + r) & 15)];
-                        } else {
-#pragma unroll 8
-                            for (int r = r0; r < rows_in; r += 2) ((uint16_t*)o.y)[first + r * o.ldy] = round16(turned[r * 16 + ((c + r) & 15)], o.type);
-                        }
-                    }
-                }
-            }
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&acc_empty[acc]));
-        }
-        if (lane == 0) tma_store_wait();
-        __syncwarp();
+    } else if (warp >= 4) {
+        ok = scale_and_store<BN, Shape::accs, 1>(a, tm_y, tm_y_rest, smem_raw, staging, column, tmem, smem_u32(acc_full), smem_u32(acc_empty), warp, lane, blockIdx.x, gridDim.x, tiles, 0);
     }
     if (!ok) drain_after_error();
     tc_fence_before_sync();
@@ -307,17 +328,129 @@ __global__ void __launch_bounds__(kTilesThreads, 1) int8_tiles_kernel(const __gr
     if (warp == 2) tmem_dealloc(tmem, Shape::cols);
 }
 
+// ---- many tokens, deep K: two SMs to a tile -----------------------------------------------------------------------
+// A cluster of two blocks works on tiles of 256 rows x 256 columns: each holds half of the rows and half of the weights of a slice, one multiplication
+// (cta_group::2, issued by the first block) uses both halves of both, and each block's tensor memory receives its rows.  A block's
+// copies per slice are 32 KB instead of 48 KB, which leaves room for six stages instead of four.
+constexpr int kPairStages = 6, kPairGroups = 2, kPairThreads = 128 + 128 * kPairGroups, kPairStageBytes = 2 * kTile * kSlice;
+constexpr size_t kPairSmem = kSmemAlign + 4 * kPairGroups * kPieceBytes + kPairStages * kPairStageBytes;
+
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_slot, uint32_t n_cols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_slot), "r"(n_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t n_cols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(n_cols) : "memory");
+}
+// Into this block's shared memory, completion on a barrier of either block (a cluster address)
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrive on the barrier at this place of both blocks once all multiplications issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1) int8_pair_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_y_rest, const TilesArgs a)
+{
+    constexpr int BN = 256, kAccs = 2;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t staging = (smem_u32(smem_raw) + kSmemAlign - 1) & ~(uint32_t)(kSmemAlign - 1), ring = staging + 4 * kPairGroups * kPieceBytes;
+    // full, acc_empty: the first block's are used; empty, acc_full: each block's own
+    __shared__ __align__(8) uint64_t full[kPairStages], empty[kPairStages], acc_full[kAccs], acc_empty[kAccs];
+    __shared__ uint32_t tmem_slot;
+    __shared__ __align__(16) float column[kPairGroups * 4 * BN];
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, rank = blockIdx.x & 1;
+    if (warp == 2) tmem_alloc_pair(smem_u32(&tmem_slot), kAccs * BN);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairStages; ++i) { mbar_init(smem_u32(&full[i]), 1); mbar_init(smem_u32(&empty[i]), 1); }
+        for (int i = 0; i < kAccs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1); mbar_init(smem_u32(&acc_empty[i]), 2 * 4 * (kPairGroups / a.slots)); }
+        fence_barrier_init();
+        prefetch_map(&tm_x); prefetch_map(&tm_w);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync();                             // both blocks' barriers are there
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tiles = a.m_tiles * a.n_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    bool ok = true;
+    if (warp == 0) {                            // producer of this block's halves
+        if (elect_one()) {
+            uint32_t stage = 0, phase = 1;
+            for (int t = first; t < tiles && ok; t += step) {
+                const int m0 = (t / a.n_tiles * 2 + rank) * a.tile_m, n0 = t % a.n_tiles * BN + rank * (BN / 2);
+                for (int s = 0; s < a.slices; ++s) {
+                    ok = mbar_wait_from(false, smem_u32(&empty[stage]), phase, a.err, kWaitEmpty);
+                    if (!ok) break;
+                    const uint32_t bar = cluster_address(smem_u32(&full[stage]), 0), dst = ring + stage * kPairStageBytes;
+                    if (rank == 0) mbar_expect_tx(smem_u32(&full[stage]), 2 * (a.tile_m + BN / 2) * kSlice + (t == first && s == 0 ? a.stall : 0u));
+                    tma_load_2d_pair(dst, &tm_x, bar, s * kSlice, m0);
+                    tma_load_2d_pair(dst + kTile * kSlice, &tm_w, bar, s * kSlice, n0);
+                    if (++stage == kPairStages) { stage = 0; phase ^= 1; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1 && rank == 0) {        // issuer for both
+        if (elect_one()) {
+            constexpr uint32_t idesc = instr_desc_i8(2 * kTile, BN);
+            const uint64_t desc0 = smem_desc(ring, 16, 1024);
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 1;
+            bool ready = false;
+            for (int t = first; t < tiles && ok; t += step) {
+                ok = mbar_wait_from(false, smem_u32(&acc_empty[acc]), acc_phase, a.err, kWaitDone);
+                if (!ok) break;
+                for (int s = 0; s < a.slices; ++s) {
+                    ok = mbar_wait_from(ready, smem_u32(&full[stage]), phase, a.err, kWaitFull);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t now = stage;
+                    if (++stage == kPairStages) { stage = 0; phase ^= 1; }
+                    ready = mbar_try_wait(smem_u32(&full[stage]), phase);
+                    const uint64_t da = desc0 + now * (kPairStageBytes >> 4), db = da + (kTile * kSlice >> 4);
+#pragma unroll
+                    for (int k = 0; k < kSlice / 32; ++k) umma_i8_pair(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, (s | k) != 0);
+                    umma_commit_pair(smem_u32(&empty[now]));
+                }
+                if (!ok) break;
+                umma_commit_pair(smem_u32(&acc_full[acc]));
+                if (++acc == kAccs) { acc = 0; acc_phase ^= 1; }
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        ok = scale_and_store<BN, kAccs, 2>(a, tm_y, tm_y_rest, smem_raw, staging, column, tmem, smem_u32(acc_full), cluster_address(smem_u32(acc_empty), 0), warp, lane, first, step, tiles, rank);
+    }
+    if (!ok) drain_after_error();
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync();                             // nobody leaves while the other block's copies, multiplications or arrivals may still reach it
+    tc_fence_after_sync();
+    if (warp == 2) tmem_dealloc_pair(tmem, kAccs * BN);
+}
+
 // ---- few tokens --------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 192;              // four warps that store, producer, issuer
 constexpr int kMaxSplitStages = 8, kMaxSplits = 8;
 struct SplitArgs { Out out; int slices, splits, stages; unsigned int* err; uint32_t stall; };
 
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ int4 load_cluster(uint32_t addr, uint32_t rank)
 {
-    uint32_t at; int4 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(cluster_address(addr, rank)) : "memory");
     return v;
 }
 // Four channels of a token; where rows of y are aligned and hold all four, one store
@@ -517,7 +650,7 @@ cudaError_t device_for(int index, Device** out)
     *out = &d;
     if (d.ready) return cudaSuccess;
     cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, index);
-    for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>,
+    for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>, (const void*)int8_pair_kernel,
                           (const void*)int8_split_kernel<16>, (const void*)int8_split_kernel<32>, (const void*)int8_split_kernel<64>, (const void*)int8_split_kernel<128>})
         if (e == cudaSuccess) e = allow_shared_memory(k);
     if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
@@ -567,17 +700,19 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     char msg[160] = "";
     CUtensorMap tx, tw;
     const int slices = (int)((p.K + kSlice - 1) / kSlice);
-    // What the forms would take, in microseconds: launch and ends, then for each round of tiles the slices and what storing adds, fitted to 36 shapes
-    // from 1 x 256 x 256 to 57600 x 512 x 256 that both were run on (off by 20 per cent at most; 16 x 4096 x 4096: 6.3 measured for clusters, 9.7 for
-    // tiles of 64 columns; 128 x 4096 x 4096: 12 and 10; 4096 x 1024 x 1024: 11.4, 8.7 and 7.5 for tiles of 64, 128 and 256 columns).
-    const auto tiles_time = [&](int columns) {
-        const double slice = columns == 64 ? 0.20 : columns == 128 ? 0.22 : 0.33, store = columns / 160.0;
-        const int64_t tiles = (p.M + kTile - 1) / kTile * ((p.N + columns - 1) / columns), rounds = (tiles + d->sms - 1) / d->sms;
+    // What the forms would take, in microseconds: launch and ends, then for each round of tiles the slices and what storing adds, fitted to 40 shapes
+    // from 1 x 256 x 256 to 57600 x 512 x 256 that several were run on (off by 20 per cent at most; 16 x 4096 x 4096: 6.3 measured for clusters, 9.7
+    // for tiles of 64 columns; 128 x 4096 x 4096: 12 and 10; 4096 x 1024 x 1024: 11.4, 8.7 and 7.5 for tiles of 64, 128 and 256 columns;
+    // 8192 x 4096 x 4096: 99.6 for tiles of 256 columns, 87 for pairs of SMs; 57600 x 512 x 256: 18.8 and 25).
+    const auto time_of = [&](int rows, int columns, int at_once, double slice, double store) {
+        const int64_t tiles = (p.M + rows - 1) / rows * ((p.N + columns - 1) / columns), rounds = (tiles + at_once - 1) / at_once;
         return 3.3 + (double)rounds * (slices * slice + store);
     };
+    const auto tiles_time = [&](int columns) { return time_of(kTile, columns, d->sms, columns == 64 ? 0.20 : columns == 128 ? 0.22 : 0.34, columns / 160.0); };
     int bn = 64;
     for (int columns : {128, 256})
         if (tiles_time(columns) < tiles_time(bn)) bn = columns;
+    const bool pair = d->sms >= 2 && time_of(2 * kTile, 256, d->sms / 2, 0.30, 2.3) < tiles_time(bn);
     const int bt = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
     const int64_t n_split_tiles = (p.N + kTile - 1) / kTile;
     // As many blocks to a tile as the SMs allow (a few more blocks than SMs are let in: two of them fit one), with two slices of K each at least
@@ -605,30 +740,45 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
         return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
     }
     TilesArgs a;
-    a.out = o; a.n_tiles = (int)((p.N + bn - 1) / bn); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
+    const int tile_n = pair ? 256 : bn, box_n = pair ? 128 : bn;        // columns of a tile, and of what one block fetches of it
+    a.out = o; a.n_tiles = (int)((p.N + tile_n - 1) / tile_n); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
     // Rows of a tile: 128, or fewer where as many rounds of tiles then fill all SMs evenly.  (57600 x 512 x 256: 450 tiles of 128 rows are 3.04
     // rounds of 148, the fourth nearly empty; tiles of 98 rows fill four.)
     const auto even_rows = [&](int64_t per_round) {
         const int64_t rounds = ((p.M + kTile - 1) / kTile + per_round - 1) / per_round;
         return (int)std::min<int64_t>(kTile, (p.M + rounds * per_round - 1) / (rounds * per_round));
     };
-    const auto shape = [&](auto f) { return bn == 64 ? f(TilesShape<64>()) : bn == 128 ? f(TilesShape<128>()) : f(TilesShape<256>()); };
-    // The weights of a block's columns stay in shared memory where they leave room for three stages of tokens and a block has two tiles at least
-    const int64_t columns = d->sms / a.n_tiles;          // blocks that share the same weights
-    const int kept_stages = shape([&](auto q) { return q.stages(slices, true, kMaxGroups); });
-    a.resident = slices <= kMaxResident && kept_stages >= 3 && columns * a.n_tiles * 10 >= d->sms * 9 && (p.M + kTile - 1) / kTile >= 2 * columns;
-    if (a.resident) a.tile_m = even_rows(columns);
-    else {
-        const int64_t rounds = ((p.M + kTile - 1) / kTile * a.n_tiles + d->sms - 1) / d->sms, most = rounds * d->sms / a.n_tiles;
-        a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
+    int64_t blocks;
+    size_t bytes;
+    if (pair) {
+        const int64_t pairs = d->sms / 2, rounds = ((p.M + 2 * kTile - 1) / (2 * kTile) * a.n_tiles + pairs - 1) / pairs, most = std::max<int64_t>(1, rounds * pairs / a.n_tiles);
+        a.tile_m = (int)std::min<int64_t>(kTile, (p.M + 2 * most - 1) / (2 * most));
+        a.m_tiles = (int)((p.M + 2 * a.tile_m - 1) / (2 * a.tile_m));
+        const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+        blocks = 2 * std::min(tiles, pairs);
+        a.stages = kPairStages; a.resident = 0; a.groups = kPairGroups; a.slots = 2 * tiles <= blocks ? 1 : 2;
+        bytes = kPairSmem;
+    } else {
+        const auto shape = [&](auto f) { return bn == 64 ? f(TilesShape<64>()) : bn == 128 ? f(TilesShape<128>()) : f(TilesShape<256>()); };
+        // The weights of a block's columns stay in shared memory where they leave room for three stages of tokens and a block has two tiles at least
+        const int64_t columns = d->sms / a.n_tiles;          // blocks that share the same weights
+        const int kept_stages = shape([&](auto q) { return q.stages(slices, true, kMaxGroups); });
+        a.resident = slices <= kMaxResident && kept_stages >= 3 && columns * a.n_tiles * 10 >= d->sms * 9 && (p.M + kTile - 1) / kTile >= 2 * columns;
+        if (a.resident) a.tile_m = even_rows(columns);
+        else {
+            const int64_t rounds = ((p.M + kTile - 1) / kTile * a.n_tiles + d->sms - 1) / d->sms, most = rounds * d->sms / a.n_tiles;
+            a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
+        }
+        a.m_tiles = (int)((p.M + a.tile_m - 1) / a.tile_m);
+        // Four groups that store where their staging leaves the ring four stages (three beside resident weights), else two
+        a.groups = kMaxGroups;
+        a.stages = a.resident ? kept_stages : shape([&](auto q) { return q.stages(slices, false, kMaxGroups); });
+        if (!a.resident && a.stages < 4) { a.groups = 2; a.stages = shape([&](auto q) { return q.stages(slices, false, 2); }); }
+        const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+        blocks = std::min<int64_t>(tiles, a.resident ? columns * a.n_tiles : d->sms);
+        a.slots = tiles <= blocks ? 1 : shape([&](auto q) { return std::min(a.groups, q.accs); });
+        bytes = shape([&](auto q) { return (size_t)q.bytes(slices, a.stages, a.resident, a.groups); });
     }
-    a.m_tiles = (int)((p.M + a.tile_m - 1) / a.tile_m);
-    // Four groups that store where their staging leaves the ring four stages (three beside resident weights), else two
-    a.groups = kMaxGroups;
-    a.stages = a.resident ? kept_stages : shape([&](auto q) { return q.stages(slices, false, kMaxGroups); });
-    if (!a.resident && a.stages < 4) { a.groups = 2; a.stages = shape([&](auto q) { return q.stages(slices, false, 2); }); }
-    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles, blocks = std::min<int64_t>(tiles, a.resident ? columns * a.n_tiles : d->sms);
-    a.slots = tiles <= blocks ? 1 : shape([&](auto q) { return std::min(a.groups, q.accs); });
     CUtensorMap ty = {}, ty_rest = {};               // of 32 rows, and of the rows that a tile has beyond multiples of 32
     if (o.wide) {
         const uint64_t dims[2] = {(uint64_t)p.N, (uint64_t)p.M}, strides[1] = {(uint64_t)(p.M == 1 ? (p.N * size + 15) / 16 * 16 : p.ldy * size)};
@@ -638,11 +788,10 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
             !encode_tensor_map(&ty_rest, type, CU_TENSOR_MAP_SWIZZLE_64B, p.y, 2, dims, strides, rest, msg, sizeof msg, "y"))
             return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
     }
-    if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, bn, msg, sizeof msg, "w"))
+    if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, a.tile_m, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, box_n, msg, sizeof msg, "w"))
         return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
-    const size_t bytes = shape([&](auto q) { return (size_t)q.bytes(slices, a.stages, a.resident, a.groups); });
     const auto go = [&](auto kernel) { return launch_early(pdl_enabled(), kernel, dim3((unsigned)blocks), dim3(128 + 128 * a.groups), bytes, s, tx, tw, ty, ty_rest, a); };
-    e = bn == 64 ? go(int8_tiles_kernel<64>) : bn == 128 ? go(int8_tiles_kernel<128>) : go(int8_tiles_kernel<256>);
+    e = pair ? go(int8_pair_kernel) : bn == 64 ? go(int8_tiles_kernel<64>) : bn == 128 ? go(int8_tiles_kernel<128>) : go(int8_tiles_kernel<256>);
     return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
 }
 

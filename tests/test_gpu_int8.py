@@ -177,7 +177,8 @@ def test_products(m, n, k):
 # shapes that each width of tile, with and without weights that stay, one round and several, two and four groups that store, and each token count of
 # the cluster form is taken for
 @pytest.mark.parametrize("m,n,k", [(30, 4096, 2048), (60, 4100, 4096), (100, 1000, 300), (16, 130, 8192), (3, 20000, 256), (9000, 64, 700), (20011, 384, 384),
-                                   (4100, 1024, 1024), (30000, 256, 512), (30001, 250, 1024), (4099, 4096, 512), (3001, 5000, 2500), (2048, 2304, 3000)])
+                                   (4100, 1024, 1024), (30000, 256, 512), (30001, 250, 1024), (4099, 4096, 512), (3001, 5000, 2500), (2048, 2304, 3000),
+                                   (8193, 700, 4096), (300, 20000, 2048), (4097, 4095, 4100)])
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_products_of_every_form(m, n, k, kind):
     check_matmul(m, n, k, kind, relu=True, seed=k)
@@ -276,7 +277,7 @@ def test_refusals():
     assert torch.equal(y.cpu(), ref_matmul(x, s, x, s, None, False, "f32"))
 
 
-@pytest.mark.parametrize("m,n,k", [(300, 200, 1024), (4, 1000, 4096)])
+@pytest.mark.parametrize("m,n,k", [(300, 200, 1024), (4, 1000, 4096), (4096, 4096, 4096)])
 def test_a_wait_that_runs_out_is_reported(m, n, k, monkeypatch):
     """The first stage of every block expects bytes that never come: the waits give up, and the next call says so."""
     x, w, sx, sw, y = matrix(m, k, 0), matrix(n, k, 1), torch.ones(m, device="cuda"), torch.ones(n, device="cuda"), torch.zeros(m, n, device="cuda")
