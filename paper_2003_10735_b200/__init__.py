@@ -524,6 +524,13 @@ def _pointers(tensors, sizes, names, what: str):
         return None
     if len(tensors) != len(sizes):
         raise ValueError(f"{what}: {len(tensors)} tensors, need {len(sizes)}")
+    try:        # all at once where they are tensors of the right types; what is wrong, or None among them, is found one by one
+        kinds = [t.dtype for t in tensors]
+        if len(set(kinds)) == 1 and len(set(names)) == 1 and (_NAME_OF.get(kinds[0]) or _name_of(kinds[0])) == names[0] \
+                and [t.numel() for t in tensors] == sizes and all([t.is_contiguous() for t in tensors]):
+            return (ctypes.c_void_p * len(sizes))(*[t.data_ptr() for t in tensors])
+    except (AttributeError, TypeError):
+        pass
     return (ctypes.c_void_p * len(sizes))(*map(_ptr, tensors, names, sizes, itertools.repeat(what)))
 
 
@@ -588,13 +595,13 @@ def st_adamw_step(opt: _AdamW, grad_scale: float = 1.0, norm_out=None) -> None:
 
 def st_adamw_read_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
     """The moments as float32 values into lists of CUDA tensors (an entry or a list may be None)."""
-    names = itertools.repeat("float32")
+    names = ["float32"] * len(opt.sizes)
     _check_adamw(load_library().st_adamw_read_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
                                                       _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
 
 
 def st_adamw_write_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
-    names = itertools.repeat("float32")
+    names = ["float32"] * len(opt.sizes)
     _check_adamw(load_library().st_adamw_write_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
                                                        _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
 

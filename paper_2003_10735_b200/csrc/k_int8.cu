@@ -150,6 +150,69 @@ __device__ __forceinline__ void stage_and_store(const float (&v)[32], uint32_t p
     }
 }
 
+// A warp's 32 rows x 32 columns to rows of y at any address: turned round in shared memory (2 KB), so that a warp's store is a piece of a row.
+// (30000 x 300 x 300: 157 us with each lane storing its own row value by value.)  fp32: 16 rows at a time, 128 bytes to a store
+__device__ __forceinline__ void store_rows_32(const float (&v)[32], float* buf, int lane, float* y, int64_t ldy, int rows)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        __syncwarp();
+        if (lane / 16 == h) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) buf[(lane & 15) * 32 + ((j + lane) & 31)] = v[j];
+        }
+        __syncwarp();
+        float* to = y + 16 * h * ldy + lane;
+        const int turn = (lane + 16 * h) & 31;
+#pragma unroll
+        for (int r = 0; r < 16; ++r, to += ldy)
+            if (16 * h + r < rows) *to = buf[r * 32 + ((turn + r) & 31)];
+    }
+    __syncwarp();
+}
+// 16 bits: two rows to a store, in words of two values; a row that begins between two words is moved by one value and its ends are stored alone
+__device__ __forceinline__ void store_rows_16(const float (&v)[32], uint32_t* buf, int lane, uint16_t* y, int64_t ldy, int rows, int type)
+{
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const uint32_t w = type == ST_BF16 ? round16x2(v[2 * k], v[2 * k + 1], ST_BF16) : round16x2(v[2 * k], v[2 * k + 1], ST_F16);
+        buf[lane * 16 + ((k + lane) & 15)] = w;
+    }
+    __syncwarp();
+    // a lane's rows are two apart: where one of them begins, to a word, the others do too
+    const int k = lane & 15, r0 = lane >> 4;
+    uint16_t* row = y + r0 * ldy;
+    const bool whole = ((uintptr_t)row & 3) == 0;
+    uint16_t* to = row + (whole ? 2 * k : 2 * k + 1);
+#pragma unroll
+    for (int i = 0; i < 16; ++i, to += 2 * ldy) {
+        const int r = r0 + 2 * i;
+        uint32_t w = buf[r * 16 + ((k + r) & 15)];
+        const uint32_t after = whole ? 0u : buf[r * 16 + ((k + 1 + r) & 15)];
+        if (r >= rows) continue;
+        if (whole || k < 15) *(uint32_t*)to = whole ? w : __byte_perm(w, after, 0x5432);
+        else { to[0] = (uint16_t)(w >> 16); to[-31] = (uint16_t)after; }              // word 15's end, and round to word 0
+    }
+    __syncwarp();
+}
+// The last columns of y, fewer than 32: 16 at a time
+__device__ __forceinline__ void store_end(const float (&v)[32], float* buf, int lane, const Out& o, int64_t first, int rows, int columns)
+{
+    const int r0 = lane / 16, c = lane % 16;
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) buf[lane * 16 + ((j + lane) & 15)] = v[h + j];
+        __syncwarp();
+        if (h + c < columns)
+#pragma unroll 1
+            for (int r = r0; r < rows; r += 2) put_one(o, first + r * o.ldy + h + c, buf[r * 16 + ((c + r) & 15)]);
+    }
+    __syncwarp();
+}
+
 // What the groups of warps that store do.  `rank` of BLOCKS that share a tile: the tile's rows are split between them.  acc_full: this block's barriers;
 // acc_empty: those of the block that issues (cluster addresses where it may be another).  False: a wait gave up.
 template <int BN, int ACCS, int BLOCKS>
@@ -205,27 +268,12 @@ __device__ __forceinline__ bool scale_and_store(const TilesArgs& a, const CUtens
                 else if (o.type == ST_F16) stage_and_store<ST_F16>(v, piece, lane, tm_out, at_col, at_row, o.N);
                 else stage_and_store<ST_F32>(v, piece, lane, tm_out, at_col, at_row, o.N);
             } else {
-                // rows of y at any address: turned round in shared memory, so that a warp's store is a piece of a row (30000 x 300 x 300:
-                // 157 us with each lane storing its own row value by value, 30 in this way)
-                if (lane == 0) tma_store_wait_read<0>();
-                float* turned = (float*)(smem_raw + (piece - smem_u32(smem_raw)));
-                const int r0 = lane / 16, c = lane % 16;
-#pragma unroll
-                for (int h = 0; h < 32; h += 16) {
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) turned[lane * 16 + ((j + lane) & 15)] = v[h + j];
-                    __syncwarp();
-                    const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0 + h + c;
-                    if (n0 + c0 + h + c >= o.N) continue;
-                    if (o.type == ST_F32) {
-#pragma unroll 8
-                        for (int r = r0; r < rows_in; r += 2) ((float*)o.y)[first + r * o.ldy] = turned[r * 16 + ((c + r) & 15)];
-                    } else {
-#pragma unroll 8
-                        for (int r = r0; r < rows_in; r += 2) ((uint16_t*)o.y)[first + r * o.ldy] = round16(turned[r * 16 + ((c + r) & 15)], o.type);
-                    }
-                }
+                if (lane == 0) tma_store_wait_read<0>();            // the copy of columns before these
+                uint32_t* buf = (uint32_t*)(smem_raw + (piece - smem_u32(smem_raw)));
+                const int64_t first = ((int64_t)m0 + quarter * 32) * o.ldy + n0 + c0;
+                if (n0 + c0 + 32 > o.N) store_end(v, (float*)buf, lane, o, first, rows_in, o.N - n0 - c0);
+                else if (o.type == ST_F32) store_rows_32(v, (float*)buf, lane, (float*)o.y + first, o.ldy, rows_in);
+                else store_rows_16(v, buf, lane, (uint16_t*)o.y + first, o.ldy, rows_in, o.type);
             }
         }
         tc_fence_before_sync();
@@ -770,10 +818,11 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
             a.tile_m = (int)std::min<int64_t>(kTile, (p.M + most - 1) / most);
         }
         a.m_tiles = (int)((p.M + a.tile_m - 1) / a.tile_m);
-        // Four groups that store where their staging leaves the ring four stages (three beside resident weights), else two
+        // Four groups that store where their staging leaves the ring four stages (three beside resident weights, or where rows of y at any address
+        // make storing the slower part: 3751 x 653 x 6518), else two
         a.groups = kMaxGroups;
         a.stages = a.resident ? kept_stages : shape([&](auto q) { return q.stages(slices, false, kMaxGroups); });
-        if (!a.resident && a.stages < 4) { a.groups = 2; a.stages = shape([&](auto q) { return q.stages(slices, false, 2); }); }
+        if (!a.resident && a.stages < (o.wide ? 4 : 3)) { a.groups = 2; a.stages = shape([&](auto q) { return q.stages(slices, false, 2); }); }
         const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
         blocks = std::min<int64_t>(tiles, a.resident ? columns * a.n_tiles : d->sms);
         a.slots = tiles <= blocks ? 1 : shape([&](auto q) { return std::min(a.groups, q.accs); });

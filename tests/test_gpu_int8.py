@@ -193,6 +193,14 @@ def test_products_of_any_layout(m, n, k, kind):
     check_matmul(m, n, k, kind, shift_x=16, shift_w=48, py=-(-n // 16) * 16)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+@pytest.mark.parametrize("pitch", [331, 332, 334, 345])
+def test_rows_of_y_at_every_alignment(kind, shift, pitch):
+    check_matmul(1000, 331, 200, kind, py=pitch, shift_y=shift, relu=True)
+    check_matmul(3000, 300, 2100, kind, py=pitch, shift_y=shift)        # columns behind y's end stay
+
+
 def test_sums_at_the_end_of_the_integers():
     """K = 131071 products of (-128)^2: the largest sum that 32 bits hold."""
     for m, n in ((1, 3), (130, 20), (300, 300)):
