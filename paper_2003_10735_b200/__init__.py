@@ -8,8 +8,8 @@ no fallback: if the CUDA library has not been built the first call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
-import itertools
 import os
 from typing import Optional
 
@@ -519,19 +519,23 @@ def _dtype_name(t, what: str) -> str:
 
 
 def _pointers(tensors, sizes, names, what: str):
-    """Array of the tensors' addresses (a None among them is NULL); None for None."""
+    """The tensors' addresses (a None among them is NULL); None for None."""
     if tensors is None:
         return None
     if len(tensors) != len(sizes):
         raise ValueError(f"{what}: {len(tensors)} tensors, need {len(sizes)}")
     try:        # all at once where they are tensors of the right types; what is wrong, or None among them, is found one by one
-        kinds = [t.dtype for t in tensors]
-        if len(set(kinds)) == 1 and len(set(names)) == 1 and (_NAME_OF.get(kinds[0]) or _name_of(kinds[0])) == names[0] \
-                and [t.numel() for t in tensors] == sizes and all([t.is_contiguous() for t in tensors]):
-            return (ctypes.c_void_p * len(sizes))(*[t.data_ptr() for t in tensors])
+        kinds = {t.dtype for t in tensors}
+        if len(kinds) == 1 and len(set(names)) == 1 and _name_of(kinds.pop()) == names[0] and [t.numel() for t in tensors] == sizes \
+                and False not in [t.is_contiguous() for t in tensors]:
+            return array.array("Q", [t.data_ptr() for t in tensors])
     except (AttributeError, TypeError):
         pass
-    return (ctypes.c_void_p * len(sizes))(*map(_ptr, tensors, names, sizes, itertools.repeat(what)))
+    return array.array("Q", [_ptr(t, name, n, what) or 0 for t, name, n in zip(tensors, names, sizes)])
+
+
+def _address(pointers) -> Optional[int]:
+    return None if pointers is None else pointers.buffer_info()[0]
 
 
 def st_adamw_create(params, exp_avg, exp_avg_sq, grads=None, exp_avg_scale=None, exp_avg_sq_scale=None, masters=None, *,
@@ -580,7 +584,8 @@ def st_adamw_create(params, exp_avg, exp_avg_sq, grads=None, exp_avg_scale=None,
 
 def st_adamw_set_grads(opt: _AdamW, grads) -> None:
     """Where the gradients are from now on (None: leave that tensor alone); the tensors must outlive the steps that read them."""
-    _check_adamw(load_library().st_adamw_set_grads(opt.handle, _pointers(grads, opt.sizes, opt.grad_names, "grads")), opt)
+    table = _pointers(grads, opt.sizes, opt.grad_names, "grads")
+    _check_adamw(load_library().st_adamw_set_grads(opt.handle, _address(table)), opt)
     opt.grads = list(grads)
 
 
@@ -596,14 +601,14 @@ def st_adamw_step(opt: _AdamW, grad_scale: float = 1.0, norm_out=None) -> None:
 def st_adamw_read_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
     """The moments as float32 values into lists of CUDA tensors (an entry or a list may be None)."""
     names = ["float32"] * len(opt.sizes)
-    _check_adamw(load_library().st_adamw_read_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
-                                                      _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
+    m, v = _pointers(exp_avg, opt.sizes, names, "exp_avg"), _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")
+    _check_adamw(load_library().st_adamw_read_moments(opt.handle, _address(m), _address(v)), opt)
 
 
 def st_adamw_write_moments(opt: _AdamW, exp_avg=None, exp_avg_sq=None) -> None:
     names = ["float32"] * len(opt.sizes)
-    _check_adamw(load_library().st_adamw_write_moments(opt.handle, _pointers(exp_avg, opt.sizes, names, "exp_avg"),
-                                                       _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")), opt)
+    m, v = _pointers(exp_avg, opt.sizes, names, "exp_avg"), _pointers(exp_avg_sq, opt.sizes, names, "exp_avg_sq")
+    _check_adamw(load_library().st_adamw_write_moments(opt.handle, _address(m), _address(v)), opt)
 
 
 def st_adamw_step_count(opt: _AdamW) -> int:

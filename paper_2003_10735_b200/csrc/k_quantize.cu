@@ -170,12 +170,13 @@ __device__ __forceinline__ RowParts parts_of(const T* row, int cols)
 
 // W warps to a row.  ALIGNED: rows of x and q begin where whole pieces can be read and written, and cols is a multiple of V.  Otherwise the integers
 // of a row are gathered in shared memory and written from there in aligned words, whatever the alignment of x's and q's rows.
-// KEEP: a row fits kItems pieces per lane; otherwise it is read twice, the second time in stretches of that many.
-// Pieces a lane keeps, and blocks an SM should hold.  Where pieces go straight to q, many small blocks are best (8192 x 4096 bf16: 21.0 us with four
-// pieces and six blocks, 24.8 with eight and three); rows that go through shared memory want fewer warps to wait for (4099 x 1111: 9.0 with eight, 13).
+// KEEP: a row's pieces stay in registers, kItems of them per lane; otherwise it is read twice, the second time in stretches of that many.
+// Pieces of a lane's stretch, and blocks an SM should hold.  Where pieces go straight to q they stay in registers, and many small blocks are best (8192 x
+// 4096 bf16: 21.0 us with four pieces and six blocks, 24.8 with eight and three).  Rows that go through shared memory are read again from
+// L1 instead (23890 x 3259 fp32: 135 us; 238 with eight pieces in registers and half of the warps).
 constexpr int kItemsStraight = 4, kItemsGathered = 8;
 template <typename T, int W, bool ALIGNED, bool KEEP>
-__global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 2) quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride,
+__global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 4) quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride,
                                                                  int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale)
 {
     constexpr int V = Piece<T>::V, kLanes = 32 * W, kItems = ALIGNED ? kItemsStraight : kItemsGathered, kRows = kThreads / kLanes, kStretch = kItems * kLanes;     // pieces
@@ -387,6 +388,46 @@ __global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(co
     }
 }
 
+// The same where blocks of whole rows would leave most SMs idle (74 rows x 4332 columns: 170 us): a block takes kSlab columns of its rows.  First the largest
+// |x| of every row, as bits in `scale`, joined with atomicMax (whose order does not matter); then the integers; then the scales.
+template <typename T>
+__global__ void __launch_bounds__(32 * kPlaneWarps) plane_tops_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride, uint32_t* __restrict__ tops)
+{
+    __shared__ uint32_t top[32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, end = min(cols, (int)(blockIdx.y + 1) * kSlab);
+    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    if (warp == 0) top[lane] = 0;
+    __syncthreads();
+    Top<T> mine;
+    if (row < rows)
+#pragma unroll 8
+        for (int c = blockIdx.y * kSlab + warp; c < end; c += kPlaneWarps) mine.add(x[row * row_stride + c * col_stride]);
+    atomicMax(&top[lane], mine.bits());
+    __syncthreads();
+    if (warp == 0 && row < rows) atomicMax(tops + row, top[lane]);
+}
+template <typename T>
+__global__ void __launch_bounds__(32 * kPlaneWarps) plane_integers_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride,
+                                                                          int8_t* __restrict__ q, int64_t ldq, const uint32_t* __restrict__ tops)
+{
+    __shared__ uint8_t turned[32 * kSlabPitch];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, begin = blockIdx.y * kSlab, n = min(cols - begin, kSlab);
+    const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
+    if (row < rows) {
+        const RowScale r = row_scale(tops[row]);
+#pragma unroll 4
+        for (int c = warp; c < n; c += kPlaneWarps) turned[lane * kSlabPitch + c] = quantize_one(x + row * row_stride + (begin + c) * col_stride, r);
+    }
+    __syncthreads();
+    for (int i = warp; i < 32 && row0 + i < rows; i += kPlaneWarps)
+        for (int c = lane; c < n; c += 32) q[(row0 + i) * ldq + begin + c] = (int8_t)turned[i * kSlabPitch + c];
+}
+__global__ void plane_scales_kernel(float* scale, int64_t rows)
+{
+    const int64_t row = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (row < rows) scale[row] = row_scale(__float_as_uint(scale[row])).scale;
+}
+
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 template <typename T>
@@ -397,6 +438,15 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
     if (cs != 1 && cols > 1) {
         const int words = aligned(q, 4) && (ldq % 4 == 0 || rows == 1);
         constexpr int per = 32 * 8 / sizeof(T);
+        if (n > kSlab && (rows + per - 1) / per < 74) {          // fewer blocks than half of the SMs
+            const dim3 grid((unsigned)((rows + 31) / 32), (unsigned)((n + kSlab - 1) / kSlab));
+            cudaError_t e = cudaMemsetAsync(scale, 0, sizeof(float) * rows, s);
+            if (e != cudaSuccess) return e;
+            plane_tops_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, (uint32_t*)scale);
+            plane_integers_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, q, ldq, (const uint32_t*)scale);
+            plane_scales_kernel<<<(unsigned)((rows + 255) / 256), 256, 0, s>>>(scale, rows);
+            return cudaGetLastError();
+        }
         const auto go = [&](auto kernel, const T* from, int64_t first, int64_t count) {
             return launch_early(early, kernel, dim3((unsigned)((count + per - 1) / per)), dim3(32 * kPlaneWarps), 0, s, from, count, n, rs, cs, q + first * ldq, ldq, scale + first, words);
         };
@@ -414,7 +464,7 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
         const int per = kThreads / 32 / warps;
         return launch_early(early, kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kThreads), 0, s, x, rows, n, rs, q, ldq, scale);
     };
-    // as few warps to a row as hold it in registers
+    // as few warps to a row as have it in one stretch
     const int64_t room = 32 * (whole ? kItemsStraight : kItemsGathered) * V;
     if (whole) {
         if (cols <= room) return go(quantize_rows_kernel<T, 1, true, true>, 1);
@@ -423,10 +473,9 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
         if (cols <= 8 * room) return go(quantize_rows_kernel<T, 8, true, true>, 8);
         return go(quantize_rows_kernel<T, 8, true, false>, 8);
     }
-    if (cols <= room) return go(quantize_rows_kernel<T, 1, false, true>, 1);
-    if (cols <= 2 * room) return go(quantize_rows_kernel<T, 2, false, true>, 2);
-    if (cols <= 4 * room) return go(quantize_rows_kernel<T, 4, false, true>, 4);
-    if (cols <= 8 * room) return go(quantize_rows_kernel<T, 8, false, true>, 8);
+    if (cols <= room) return go(quantize_rows_kernel<T, 1, false, false>, 1);
+    if (cols <= 2 * room) return go(quantize_rows_kernel<T, 2, false, false>, 2);
+    if (cols <= 4 * room) return go(quantize_rows_kernel<T, 4, false, false>, 4);
     return go(quantize_rows_kernel<T, 8, false, false>, 8);
 }
 

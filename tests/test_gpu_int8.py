@@ -72,7 +72,7 @@ def test_rows_of_tokens(kind, rows, cols):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("cols,h,w", [(1, 5, 7), (4, 8, 8), (21, 11, 13), (256, 9, 32), (255, 3, 21), (257, 6, 11), (300, 1, 33), (1000, 2, 17)])
+@pytest.mark.parametrize("cols,h,w", [(1, 5, 7), (4, 8, 8), (21, 11, 13), (256, 9, 32), (255, 3, 21), (257, 6, 11), (300, 1, 33), (1000, 2, 17), (4333, 3, 25), (700, 40, 130), (5000, 1, 1)])
 def test_pixels_of_planar_maps(kind, cols, h, w):
     torch.manual_seed(cols)
     planes = (torch.randn(cols, h, w, device="cuda") * 3).relu().to(TYPES[kind])
