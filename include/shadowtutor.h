@@ -432,7 +432,7 @@ ST_API st_status st_adamw_set_lr(st_adamw *opt, double lr);
  * st_adamw_step — one step on all tensors: one kernel, and one more in front of it that measures the gradients' norm where max_norm,
  * skip_nonfinite or norm_out asks for it.  Returns at once; may be captured into a graph.
  *   grad_scale  finite; multiplies every gradient (1 / the loss scale of fp16 training).
- *   norm_out    device, or NULL; one fp32: the norm before clipping.
+ *   norm_out    device, or NULL; one fp32: the norm before clipping.  Not part of any other buffer of the step.
  */
 ST_API st_status st_adamw_step(st_adamw *opt, float grad_scale, float *norm_out);
 

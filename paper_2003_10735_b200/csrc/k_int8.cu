@@ -772,7 +772,9 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
         a.out = o; a.slices = slices; a.splits = splits; a.err = d->err_dev; a.stall = stall_bytes();
         const int stage = (kTile + bt) * kSlice, per = (slices + splits - 1) / splits;
         a.stages = std::min({kMaxSplitStages, per, 200 * 1024 / stage});
-        const size_t bytes = (size_t)std::max(a.stages * stage, splits > 1 ? bt * kTile * 4 : 0) + kSmemAlign;
+        // At least as large a share of an SM's shared memory as its columns are of tensor memory: blocks of a cluster wait for one another, and would
+        // do so for good if clusters of several streams each held columns that another one's blocks wait for
+        const size_t bytes = std::max<size_t>((size_t)std::max(a.stages * stage, splits > 1 ? bt * kTile * 4 : 0) + kSmemAlign, (size_t)std::max(bt, 32) * (227 * 1024 / 512));
         if (!operand_map(&tx, p.x, p.M, p.ldx, p.K, bt, msg, sizeof msg, "x") || !operand_map(&tw, p.w, p.N, p.ldw, p.K, kTile, msg, sizeof msg, "w"))
             return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", msg);
         cudaLaunchConfig_t cfg = {};

@@ -438,7 +438,7 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
     if (cs != 1 && cols > 1) {
         const int words = aligned(q, 4) && (ldq % 4 == 0 || rows == 1);
         constexpr int per = 32 * 8 / sizeof(T);
-        if (n > kSlab && (rows + per - 1) / per < 74) {          // fewer blocks than half of the SMs
+        if (n > kSlab && (n + kSlab - 1) / kSlab <= 65535 && (rows + per - 1) / per < 74) {         // fewer blocks than half of the SMs
             const dim3 grid((unsigned)((rows + 31) / 32), (unsigned)((n + kSlab - 1) / kSlab));
             cudaError_t e = cudaMemsetAsync(scale, 0, sizeof(float) * rows, s);
             if (e != cudaSuccess) return e;

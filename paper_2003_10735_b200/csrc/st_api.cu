@@ -137,7 +137,7 @@ int st::fail_on_thread(int code, const char* fmt, ...)
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    g_init_error = buf;
+    try { g_init_error = buf; } catch (...) {}
     return code;
 }
 

@@ -97,9 +97,9 @@ def test_quotients_next_to_a_half():
     check_quantize(torch.from_numpy(np.ascontiguousarray(x.T)).cuda().t())
 
 
-@pytest.mark.parametrize("planar", [False, True])
-def test_rows_that_are_zero_tiny_or_not_finite(planar):
-    x = torch.randn(12, 40, device="cuda")
+@pytest.mark.parametrize("planar,cols", [(False, 40), (False, 41), (False, 5000), (True, 40), (True, 301)])
+def test_rows_that_are_zero_tiny_or_not_finite(planar, cols):
+    x = torch.randn(12, cols, device="cuda")
     x[0] = 0
     x[1] = 0; x[1, 3] = 1e-45                           # the least fp32: its scale underflows
     x[2] = x[2] * 1e-39                                 # scales that fp32 holds with few bits
@@ -229,6 +229,24 @@ def test_product_offsets_beyond_32_bits():
     st.st_int8_matmul(x, sx, w, sw, y, cuda_stream=stream())
     want = ref_matmul(x[-300:], sx[-300:], w, sw, None, False, "bf16")
     assert torch.equal(y[-300:].cpu(), want) and (y[:1000] == 0).all() and (y[m // 2:m // 2 + 1000] == 0).all()
+
+
+def test_clusters_of_several_streams_at_once():
+    """Small products whose clusters share SMs, on four streams: each block needs tensor memory before its cluster can go on."""
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    shapes = [(16, 1024, 512), (60, 1024, 4096), (100, 1024, 8192)]
+    sets = [(matrix(m, k, i), matrix(n, k, i + 5), torch.rand(m, device="cuda"), torch.rand(n, device="cuda")) for i, (m, n, k) in enumerate(shapes)]
+    ys = [[torch.zeros(m, n, device="cuda") for m, n, _ in shapes] for _ in streams]
+    st.st_int8_matmul(sets[0][0], sets[0][2], sets[0][1], sets[0][3], ys[0][0], cuda_stream=stream())
+    torch.cuda.synchronize()
+    for _ in range(40):
+        for i, ((x, w, sx, sw)) in enumerate(sets):
+            for s, y in zip(streams, ys):
+                st.st_int8_matmul(x, sx, w, sw, y[i], cuda_stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for i, (x, w, sx, sw) in enumerate(sets):
+        want = ref_matmul(x, sx, w, sw, None, False, "f32")
+        assert all(torch.equal(y[i].cpu(), want) for y in ys)
 
 
 def test_products_on_two_streams_and_replayed():
