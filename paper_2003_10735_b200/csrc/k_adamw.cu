@@ -237,7 +237,7 @@ __device__ __forceinline__ void encode(const float (&m)[kPer], const float (&roo
 // ---- which values are a block's ---------------------------------------------------------------------------------
 // Part b of a launch's parts takes the b-th share of the chunks, consecutive ones, so that the record of a tensor is read once per share and
 // what follows are addresses that need no further look-up.  (A table entry per chunk, read in turn, put two dependent loads in front of
-// each chunk's own: 38 instead of 24 us for the norm of 40 M bf16 gradients.)  The first record is read ahead of pdl_wait().
+// each chunk's own.)  The first record is read ahead of pdl_wait().
 struct Share { int64_t c, end; ChunkRec chunk; TensorRec tensor; };
 __device__ __forceinline__ Share share_of(const Plan& p, int64_t from, int64_t to, int part, int parts)
 {
@@ -476,8 +476,8 @@ __device__ __forceinline__ void step_block_8(const TensorRec* record, const Tens
 }
 
 // All whole blocks of a tensor's part; returns where it stopped.  A function of its own for each combination of types: the conversions
-// are decided outside the loop, and the registers are this loop's alone (inlined into the walk, with all combinations side by
-// side, the 8-bit step of 200 M bf16 values took 738 us instead of 545).  With 8-bit moments, where a warp has much to work out, the next
+// are decided outside the loop, and the registers are this loop's alone (inlined into the walk, the 8-bit step of 200 M bf16
+// values took 738 us with all combinations side by side and 545 with one compiled alone).  With 8-bit moments, where a warp has much to work out, the next
 // block's loads are on their way meanwhile.
 template <int BITS, int PARAM, int GRAD, bool MASTER>
 __device__ __noinline__ int64_t step_blocks(const TensorRec* record, const void* grad, StepNow k, int64_t at, int64_t end)
@@ -875,7 +875,7 @@ st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adam
     // Blocks of a launch: as many as the GPU holds at once, or one per `span` chunks where that is more.  A step with fp32 moments and the reading
     // of moments wait for memory, and short shares that the GPU hands out as blocks end keep all of it busy (150 M fp32 values with
     // spans of 4 / 8 chunks / one share per resident block: 633 / 648 / 690 us; reading 200 M values: 327 with 8, 353).  A step with 8-bit
-    // moments and the norm wait for instructions, and a block's beginning and end cost more than an uneven end (200 M: 744 us with
+    // moments and the norm have more to work out per byte, and a block's beginning and end cost more than an uneven end (200 M: 744 us with
     // spans of 8, 520 with one share each; norm 77 and 63).
     const auto blocks = [&](int per_sm, int span) {
         const int64_t resident = (int64_t)sms * std::max(per_sm, 1), most = span ? std::max(resident, n_chunks / span) : resident;
