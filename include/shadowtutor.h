@@ -464,7 +464,7 @@ ST_API const char *st_adamw_last_error(const st_adamw *opt);
  *   q           device; int8 [rows][ldq], ldq >= cols; what lies between cols and ldq is left as it is.  With ldq a multiple of 16 and q
  *               on a multiple of 16 bytes, st_int8_matmul takes its fast path.
  *   scale       device; fp32 [rows].
- *   rows, cols  rows >= 0, cols >= 1.
+ *   rows, cols  rows >= 0, cols >= 1, at most 2^31 - 1 each (ST_ERR_UNSUPPORTED above).
  * Returns after enqueueing on cuda_stream (NULL = default stream), allocates nothing, and may be captured into a graph.
  * ST_ERR_INVALID_ARG: a pointer that is not memory of the current device, unaligned to its element or overlapping q or scale; bad extents.
  */

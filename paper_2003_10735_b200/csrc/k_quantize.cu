@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 4) quantize_rows_kerne
         }
         if (!ALIGNED) {
             if (me < p.head) top.add(src[me]);
-            if (p.tail + me < cols) top.add(src[p.tail + me]);
+            if (me < cols - p.tail) top.add(src[p.tail + me]);
         }
         if (KEEP) {
 #pragma unroll
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 4) quantize_rows_kerne
         uint8_t* const buf = area + ((8 - p.head) & 7) * is_first;
         if (mine) {
             if (is_first && me < p.head) buf[me] = quantize_one(src + me, r);
-            if (is_last && p.tail + me < cols) buf[p.tail + me - first] = quantize_one(src + p.tail + me, r);
+            if (is_last && me < cols - p.tail) buf[p.tail + me - first] = quantize_one(src + p.tail + me, r);
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 const int at = begin + me + i * kLanes;
@@ -321,18 +321,18 @@ __global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(co
             at += j < last ? col_stride : 0;
         }
     };
-    for (int slab = 0; slab < cols; slab += kSlab) {
+    for (int slab = 0;; slab += kSlab) {            // cols may be 2^31 - 1: no sum goes beyond it
 #pragma unroll
         for (int i = 0; i < kGroups; ++i)
-            if (slab + 4 * (warp + kPlaneWarps * i) < cols) fetch(kept[i], slab + 4 * (warp + kPlaneWarps * i));
+            if (4 * (warp + kPlaneWarps * i) < cols - slab) fetch(kept[i], slab + 4 * (warp + kPlaneWarps * i));
 #pragma unroll
         for (int i = 0; i < kGroups; ++i)
-            if (slab + 4 * (warp + kPlaneWarps * i) < cols)
+            if (4 * (warp + kPlaneWarps * i) < cols - slab)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int u = 0; u < P; ++u) top[u].add(kept[i][j][u]);
-        if (KEEP) break;
+        if (KEEP || cols - slab <= kSlab) break;
     }
 #pragma unroll
     for (int u = 0; u < P; ++u) tops[warp][32 * u + lane] = top[u].bits();
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(co
         if (row0 + threadIdx.x < rows) scale[row0 + threadIdx.x] = r.scale;
     }
     __syncthreads();
-    for (int slab = 0; slab < cols; slab += kSlab) {
+    for (int slab = 0;; slab += kSlab) {
         const int n = min(cols - slab, kSlab);
         if (!KEEP) {
 #pragma unroll
@@ -384,35 +384,37 @@ __global__ void __launch_bounds__(32 * kPlaneWarps, 2) quantize_planes_kernel(co
                 for (int c = 4 * whole + lane; c < n; c += 32) dst[c] = (int8_t)from[c];
             }
         }
-        if (!KEEP) __syncthreads();
+        if (KEEP || cols - slab <= kSlab) break;
+        __syncthreads();
     }
 }
 
 // The same where blocks of whole rows would leave most SMs idle (74 rows x 4332 columns of bf16: 170 us, 13 in this way): a block takes kSlab columns of its rows.  First the largest
-// |x| of every row, as bits in `scale`, joined with atomicMax (whose order does not matter); then the integers; then the scales.
+// |x| of every row, as bits in `scale`, joined with atomicMax (whose order does not matter); then the integers; then the scales.  Block i: rows from
+// 32 (i % groups) and columns from kSlab (i / groups), in one extent of the grid, since only its first holds the slabs of 2^31 - 1 columns.
 template <typename T>
-__global__ void __launch_bounds__(32 * kPlaneWarps) plane_tops_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride, uint32_t* __restrict__ tops)
+__global__ void __launch_bounds__(32 * kPlaneWarps) plane_tops_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride, uint32_t* __restrict__ tops, int groups)
 {
     __shared__ uint32_t top[32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, end = min(cols, (int)(blockIdx.y + 1) * kSlab);
-    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, begin = (int)(blockIdx.x / groups) * kSlab, n = min(cols - begin, kSlab);
+    const int64_t row = (int64_t)(blockIdx.x % groups) * 32 + lane;
     if (warp == 0) top[lane] = 0;
     __syncthreads();
     Top<T> mine;
     if (row < rows)
 #pragma unroll 8
-        for (int c = blockIdx.y * kSlab + warp; c < end; c += kPlaneWarps) mine.add(x[row * row_stride + c * col_stride]);
+        for (int c = warp; c < n; c += kPlaneWarps) mine.add(x[row * row_stride + (begin + c) * col_stride]);
     atomicMax(&top[lane], mine.bits());
     __syncthreads();
     if (warp == 0 && row < rows) atomicMax(tops + row, top[lane]);
 }
 template <typename T>
 __global__ void __launch_bounds__(32 * kPlaneWarps) plane_integers_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride, int64_t col_stride,
-                                                                          int8_t* __restrict__ q, int64_t ldq, const uint32_t* __restrict__ tops)
+                                                                          int8_t* __restrict__ q, int64_t ldq, const uint32_t* __restrict__ tops, int groups)
 {
     __shared__ uint8_t turned[32 * kSlabPitch];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, begin = blockIdx.y * kSlab, n = min(cols - begin, kSlab);
-    const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, begin = (int)(blockIdx.x / groups) * kSlab, n = min(cols - begin, kSlab);
+    const int64_t row0 = (int64_t)(blockIdx.x % groups) * 32, row = row0 + lane;
     if (row < rows) {
         const RowScale r = row_scale(tops[row]);
 #pragma unroll 4
@@ -438,12 +440,13 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
     if (cs != 1 && cols > 1) {
         const int words = aligned(q, 4) && (ldq % 4 == 0 || rows == 1);
         constexpr int per = 32 * 8 / sizeof(T);
-        if (n > kSlab && (n + kSlab - 1) / kSlab <= 65535 && (rows + per - 1) / per < 74) {         // fewer blocks than half of the SMs
-            const dim3 grid((unsigned)((rows + 31) / 32), (unsigned)((n + kSlab - 1) / kSlab));
+        if (n > kSlab && (rows + per - 1) / per < 74) {         // fewer blocks than half of the SMs
+            const int groups = (int)((rows + 31) / 32);
+            const unsigned grid = (unsigned)(groups * ((cols + kSlab - 1) / kSlab));
             cudaError_t e = cudaMemsetAsync(scale, 0, sizeof(float) * rows, s);
             if (e != cudaSuccess) return e;
-            plane_tops_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, (uint32_t*)scale);
-            plane_integers_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, q, ldq, (const uint32_t*)scale);
+            plane_tops_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, (uint32_t*)scale, groups);
+            plane_integers_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, q, ldq, (const uint32_t*)scale, groups);
             plane_scales_kernel<<<(unsigned)((rows + 255) / 256), 256, 0, s>>>(scale, rows);
             return cudaGetLastError();
         }

@@ -126,6 +126,22 @@ def test_quantize_offsets_beyond_32_bits():
     assert int(q.ne(0).sum()) == int(np.count_nonzero(want_q))
 
 
+@pytest.mark.parametrize("planar", [False, True])
+def test_as_many_columns_as_a_row_may_have(planar):
+    """2^31 - 1 columns: counts of columns that are rounded up, and places of a row's last values, lie next to the end of 32-bit integers."""
+    cols = 2 ** 31 - 1
+    rows = 2 if planar else 1
+    flat = torch.zeros(rows * cols + 3, dtype=torch.bfloat16, device="cuda")
+    x = flat[3:].as_strided((rows, cols), (1, rows) if planar else (cols, 1))         # row-major: its last values lie behind the last whole piece
+    at = torch.tensor([0, 255, 256, 2 ** 30 + 5] + list(range(cols - 300, cols)), device="cuda")
+    x[:, at] = (torch.arange(1, at.numel() * rows + 1, device="cuda") % 97 - 48).view(rows, -1).to(torch.bfloat16)
+    q, scale = torch.zeros(rows, cols, dtype=torch.int8, device="cuda"), torch.zeros(rows, device="cuda")
+    st.st_quantize_rows(x, q, scale, cuda_stream=stream())
+    want_q, want_s = ref_quantize(x[:, at].double().cpu().numpy())
+    assert np.array_equal(scale.cpu().numpy(), want_s) and np.array_equal(q[:, at].cpu().numpy(), want_q)
+    assert sum(int(torch.count_nonzero(part)) for r in range(rows) for part in q[r].split(2 ** 30)) == int(np.count_nonzero(want_q))
+
+
 # ---------------------------------------------------------------------------- products
 def matrix(rows, cols, seed, pitch=None, shift=0, extremes=False):
     g = torch.Generator(device="cuda").manual_seed(seed)
