@@ -498,7 +498,8 @@ ST_API st_status st_int8_matmul(const int8_t *x, int64_t ldx, const float *x_sca
  * st_set_frozen_features stores, computed by st_int8_matmul from the layer's quantised input, without a feature map in between.
  *   x, ldx, x_scale   the layer's input, a pixel per row (feat_h * feat_w rows, row-major over the map), K channels.
  *   w, ldw, w_scale   the layer's weights, c_in rows.   bias, relu as in st_int8_matmul.
- * Works on the context's stream.  ST_ERR_UNSUPPORTED with gemm_precision 0 (the cache is then fp32 planes).
+ * Works on the context's stream.  ST_ERR_UNSUPPORTED with gemm_precision 0 (the cache is then fp32 planes).  Where a device wait gives up and leaves
+ * the cache incomplete, the context's next call that waits for the stream returns ST_ERR_CUDA.
  */
 ST_API st_status st_set_frozen_features_int8(st_ctx *ctx, int32_t stream, const int8_t *x, int64_t ldx, const float *x_scale,
                                              const int8_t *w, int64_t ldw, const float *w_scale, const float *bias,

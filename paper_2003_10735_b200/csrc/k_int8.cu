@@ -723,9 +723,7 @@ bool operand_map(CUtensorMap* m, const int8_t* q, int64_t rows, int64_t ld, int6
     return encode_tensor_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, q, 2, dims, strides, box, msg, msg_len, what);
 }
 
-}  // namespace
-
-int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
+int launch(const Int8Product& p, cudaStream_t s)
 {
     const auto cuda_fail = [](cudaError_t e) { cudaGetLastError(); return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", cudaGetErrorString(e)); };
     int index = 0;
@@ -733,11 +731,12 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     cudaError_t e = cudaGetDevice(&index);
     if (e == cudaSuccess) e = device_for(index, &d);
     if (e != cudaSuccess) return cuda_fail(e);
-    if (const unsigned int code = *(volatile unsigned int*)d->err) {
+    if (const unsigned int code = p.err ? 0u : *(volatile unsigned int*)d->err) {
         *(volatile unsigned int*)d->err = 0;
         return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of an earlier product gave up (code %u); its result is not complete", code);
     }
     Out o = {p.y, p.ldy, p.y_type, 0, p.x_scale, p.w_scale, p.bias, p.relu ? 0.f : -INFINITY, 1.f, (int)p.M, (int)p.N};
+    unsigned int* const err = p.err ? p.err : d->err_dev;
     const int64_t size = p.y_type == ST_F32 ? 4 : 2;
     o.wide = aligned(p.y, 16) && (p.M == 1 || p.ldy * size % 16 == 0);
     const bool tma = aligned(p.x, 16) && aligned(p.w, 16) && (p.M == 1 || p.ldx % 16 == 0) && (p.N == 1 || p.ldw % 16 == 0);
@@ -770,7 +769,7 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     const double weight_time = (double)p.N * (double)p.K / 5.5e6, slice_time = 0.16 * ((slices + splits - 1) / splits) * (double)((n_split_tiles * splits + d->sms - 1) / d->sms);
     if (p.M <= 128 && 2.6 + std::max(weight_time, slice_time) + 0.04 * bt < tiles_time(bn)) {
         SplitArgs a;
-        a.out = o; a.slices = slices; a.splits = splits; a.err = d->err_dev; a.stall = stall_bytes();
+        a.out = o; a.slices = slices; a.splits = splits; a.err = err; a.stall = stall_bytes();
         const int stage = (kTile + bt) * kSlice, per = (slices + splits - 1) / splits;
         a.stages = std::min({kMaxSplitStages, per, 200 * 1024 / stage});
         // At least as large a share of an SM's shared memory as its columns are of tensor memory: blocks of a cluster wait for one another, and would
@@ -792,7 +791,7 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     }
     TilesArgs a;
     const int tile_n = pair ? 256 : bn, box_n = pair ? 128 : bn;        // columns of a tile, and of what one block fetches of it
-    a.out = o; a.n_tiles = (int)((p.N + tile_n - 1) / tile_n); a.slices = slices; a.err = d->err_dev; a.stall = stall_bytes();
+    a.out = o; a.n_tiles = (int)((p.N + tile_n - 1) / tile_n); a.slices = slices; a.err = err; a.stall = stall_bytes();
     // Rows of a tile: 128, or fewer where as many rounds of tiles then fill all SMs evenly.  (57600 x 512 x 256: 450 tiles of 128 rows are 3.04
     // rounds of 148, the fourth nearly empty; tiles of 98 rows fill four.)
     const auto even_rows = [&](int64_t per_round) {
@@ -847,6 +846,32 @@ int launch_int8_matmul(const Int8Product& p, cudaStream_t s)
     return e == cudaSuccess ? (int)ST_OK : cuda_fail(e);
 }
 
+}  // namespace
+
+int int8_matmul(const Int8Product& p, cudaStream_t s)
+{
+    const int64_t M = p.M, N = p.N, K = p.K;
+    const auto bad = [](const char* what) { return fail_on_thread(ST_ERR_INVALID_ARG, "st_int8_matmul: %s", what); };
+    if (M < 0 || N < 0 || K < 1) return bad("needs M >= 0, N >= 0 and K >= 1");
+    if (p.y_type != ST_F32 && p.y_type != ST_BF16 && p.y_type != ST_F16) return bad("y_type is not an st_dtype");
+    if (p.relu & ~1) return bad("relu must be 0 or 1");
+    if (p.ldx < K || p.ldw < K || p.ldy < N) return bad("ldx, ldw below K or ldy below N");
+    if (K > kMaxInt8K) return fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: K above %d could overflow the 32-bit sums", kMaxInt8K);
+    if (M > kMaxInt8Extent - 255 || N > kMaxInt8N || !extent_fits(M, p.ldx, K, 1) || !extent_fits(N, p.ldw, K, 1) || !extent_fits(M, p.ldy, N, 1) ||
+        ((M + 127) / 128) * ((N + 63) / 64) > kMaxInt8Extent / 2)
+        return fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: extents beyond the kernels' 32-bit counts of tiles");
+    if (M == 0 || N == 0) return ST_OK;
+    Int8Buffers b("st_int8_matmul");
+    b.add("x", p.x, 1, (M - 1) * p.ldx + K, false);
+    b.add("x_scale", p.x_scale, 4, M, false);
+    b.add("w", p.w, 1, (N - 1) * p.ldw + K, false);
+    b.add("w_scale", p.w_scale, 4, N, false);
+    if (p.bias) b.add("bias", p.bias, 4, N, false);
+    b.add("y", p.y, p.y_type == ST_F32 ? 4 : 2, (M - 1) * p.ldy + N, true);
+    if (!b.ok()) return b.status();
+    return launch(p, s);
+}
+
 }  // namespace st
 
 using namespace st;
@@ -854,24 +879,5 @@ using namespace st;
 extern "C" st_status st_int8_matmul(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale,
                                     const float* bias, int32_t relu, int64_t M, int64_t N, int64_t K, void* y, int32_t y_type, int64_t ldy, void* cuda_stream)
 {
-    const auto bad = [](const char* what) { return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_int8_matmul: %s", what); };
-    if (M < 0 || N < 0 || K < 1) return bad("needs M >= 0, N >= 0 and K >= 1");
-    if (y_type != ST_F32 && y_type != ST_BF16 && y_type != ST_F16) return bad("y_type is not an st_dtype");
-    if (relu & ~1) return bad("relu must be 0 or 1");
-    if (ldx < K || ldw < K || ldy < N) return bad("ldx, ldw below K or ldy below N");
-    if (K > kMaxInt8K) return (st_status)fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: K above %d could overflow the 32-bit sums", kMaxInt8K);
-    if (M > kMaxInt8Extent - 255 || N > kMaxInt8N || !extent_fits(M, ldx, K, 1) || !extent_fits(N, ldw, K, 1) || !extent_fits(M, ldy, N, 1) ||
-        ((M + 127) / 128) * ((N + 63) / 64) > kMaxInt8Extent / 2)
-        return (st_status)fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: extents beyond the kernels' 32-bit counts of tiles");
-    if (M == 0 || N == 0) return ST_OK;
-    Int8Buffers b("st_int8_matmul");
-    b.add("x", x, 1, (M - 1) * ldx + K, false);
-    b.add("x_scale", x_scale, 4, M, false);
-    b.add("w", w, 1, (N - 1) * ldw + K, false);
-    b.add("w_scale", w_scale, 4, N, false);
-    if (bias) b.add("bias", bias, 4, N, false);
-    b.add("y", y, y_type == ST_F32 ? 4 : 2, (M - 1) * ldy + N, true);
-    if (!b.ok()) return b.status();
-    const Int8Product p = {x, ldx, x_scale, w, ldw, w_scale, bias, relu, M, N, K, y, y_type, ldy};
-    return (st_status)launch_int8_matmul(p, (cudaStream_t)cuda_stream);
+    return (st_status)int8_matmul({x, ldx, x_scale, w, ldw, w_scale, bias, relu, M, N, K, y, y_type, ldy, nullptr}, (cudaStream_t)cuda_stream);
 }

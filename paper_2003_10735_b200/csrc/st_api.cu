@@ -873,8 +873,9 @@ st_status st_set_frozen_features_int8(st_ctx* ctx, int32_t stream, const int8_t*
     st_status st = check_stream_index(ctx, stream);
     if (st != ST_OK) return st;
     if (!ctx->bf16_mode) return fail(ctx, ST_ERR_UNSUPPORTED, "st_set_frozen_features_int8: needs gemm_precision 1");
-    st = st_int8_matmul(x, ldx, x_scale, w, ldw, w_scale, bias, relu, ctx->p, ctx->Cin, K, ctx->x_bf16 + (int64_t)stream * ctx->p * ctx->Cin, ST_BF16,
-                        ctx->Cin, ctx->stream);
+    // a wait that gives up is the context's to report, like one of its own kernels'
+    st = (st_status)int8_matmul({x, ldx, x_scale, w, ldw, w_scale, bias, relu, ctx->p, ctx->Cin, K, ctx->x_bf16 + (int64_t)stream * ctx->p * ctx->Cin, ST_BF16,
+                                 ctx->Cin, ctx->bad + 2}, ctx->stream);
     if (st != ST_OK) return fail(ctx, st, "st_set_frozen_features_int8: %s", st_last_error(nullptr));
     ctx->launches += 1;
     ctx->has_feat[stream] = 1;

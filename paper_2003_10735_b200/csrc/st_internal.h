@@ -190,15 +190,17 @@ bool student_mask_fused_supported(int C);   // confusion counters fit shared mem
 cudaError_t prepare_student_mask();         // once per device, outside any stream capture
 void launch_student_mask(const StudentMaskArgs& a, cudaStream_t s);
 
-// ---- 8-bit integer products (k_int8.cu): arguments checked by the entry points; returns an st_status, the text as fail_on_thread
+// ---- 8-bit integer products (k_int8.cu)
 struct Int8Product {
     const int8_t* x; int64_t ldx; const float* x_scale;
     const int8_t* w; int64_t ldw; const float* w_scale;
     const float* bias; int relu;
     int64_t M, N, K;
     void* y; int y_type; int64_t ldy;
+    unsigned int* err;          // device word: first wait that gave up; nullptr: the one that st_int8_matmul looks after
 };
-int launch_int8_matmul(const Int8Product& p, cudaStream_t s);
+// Checks of arguments, then the launch; returns an st_status, the text as fail_on_thread
+int int8_matmul(const Int8Product& p, cudaStream_t s);
 
 // ---- fp32 CUDA-core convolutions (gemm_precision 0) -------------------------------------------
 // Planes [C][rows][pitch] with the map at row kPadTop, column kPadLeft and zeros around it (allocated zero; every writer

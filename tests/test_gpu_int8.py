@@ -381,3 +381,30 @@ def test_the_front_parts_last_layer_in_8_bits(h, w, k):
     assert ei.value.status == st.ST_ERR_UNSUPPORTED
     for c in ctxs + [plain]:
         st.st_destroy(c)
+
+
+@pytest.mark.parametrize("h,w,k", [(6, 11, 4096), (45, 80, 200)])
+def test_a_feature_cache_left_incomplete_is_the_contexts_to_report(h, w, k, monkeypatch):
+    """A wait that runs out while the feature cache is filled (few pixels: the form that splits K; many: tiles) is reported by the context's
+    next call that waits, once, and by nobody else's product."""
+    c_in, C = 64, 5
+    x, wq, sx, sw = matrix(h * w, k, 0), matrix(c_in, k, 1), torch.rand(h * w, device="cuda") * 1e-3, torch.rand(c_in, device="cuda") * 1e-2
+    y = torch.zeros(h * w, c_in, dtype=torch.bfloat16, device="cuda")
+    st.st_int8_matmul(x, sx, wq, sw, y, cuda_stream=stream())
+    ctx = st.st_init_head(c_in=c_in, n_classes=C, feat_h=h, feat_w=w, gemm_precision=1, cuda_stream=stream(),
+                          init_params=si.initial_head_params(c_in, 0, C, 1000))
+    st.st_set_labels(ctx, 0, torch.zeros(4 * h, 4 * w, dtype=torch.uint8, device="cuda"))
+    monkeypatch.setenv("ST_TEST_STALL_INT8", "1")
+    st.st_set_frozen_features_int8(ctx, 0, x, sx, wq, sw)
+    monkeypatch.delenv("ST_TEST_STALL_INT8")
+    torch.cuda.synchronize()
+    st.st_int8_matmul(x, sx, wq, sw, y, cuda_stream=stream())               # another caller's product: nothing of it gave up
+    assert torch.equal(y.cpu(), ref_matmul(x, sx, wq, sw, None, False, "bf16"))
+    with pytest.raises(st.StError) as ei:
+        st.st_distill_step(ctx, 1, np.zeros(1, np.float32))
+        st.st_read_tensor(ctx, 0, st.ST_TENSOR_FEATURES)
+    assert ei.value.status == st.ST_ERR_CUDA and "gave up waiting" in str(ei.value)
+    st.st_set_frozen_features_int8(ctx, 0, x, sx, wq, sw)
+    got = st.st_read_tensor(ctx, 0, st.ST_TENSOR_FEATURES).reshape(c_in, h * w)
+    assert np.array_equal(got, y.float().cpu().numpy().T)
+    st.st_destroy(ctx)
