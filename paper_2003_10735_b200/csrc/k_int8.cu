@@ -684,26 +684,33 @@ __global__ void __launch_bounds__(256) int8_plain_kernel(const int8_t* __restric
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-// What a device needs before its first launch: the kernels' limits of shared memory, and a word in pinned host memory in which a wait that gave up
-// leaves its code, so that the next call can tell without waiting for the device.
-struct Device { bool ready = false; int sms = 0; unsigned int *err = nullptr, *err_dev = nullptr; };
-constexpr int kMaxDevices = 64;
+// What a device needs before its first launch: the kernels' limits of shared memory, and words in pinned host memory in which a wait that gave up
+// leaves its code, so that the next call on the same stream can tell without waiting for the device.  Streams, by their handles, have words of their
+// own, up to kErrWords of them; any more share.  (Their numbers, cudaStreamGetId, cannot be asked for while they are captured.)
+constexpr int kMaxDevices = 64, kErrWords = 1024;
+struct Device { bool ready = false; int sms = 0; unsigned int *err = nullptr, *err_dev = nullptr; uintptr_t owner[kErrWords] = {}; };
 Device g_devices[kMaxDevices];
 std::mutex g_mutex;
 
-cudaError_t device_for(int index, Device** out)
+// `word`: which of the device's words is the stream's
+cudaError_t device_for(int index, cudaStream_t s, Device** out, int* word)
 {
     if (index < 0 || index >= kMaxDevices) return cudaErrorInvalidDevice;
     std::lock_guard<std::mutex> lock(g_mutex);
     Device& d = g_devices[index];
     *out = &d;
+    const uintptr_t key = (uintptr_t)s + 1;             // the default stream's handle is 0, and so is a word without an owner
+    uint32_t at = (uint32_t)((uint64_t)key * 0x9e3779b97f4a7c15u >> 54);
+    for (int i = 0; i < kErrWords && d.owner[at] != key && d.owner[at]; ++i) at = (at + 1) % kErrWords;
+    if (!d.owner[at]) d.owner[at] = key;
+    *word = (int)at;
     if (d.ready) return cudaSuccess;
     cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, index);
     for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>, (const void*)int8_pair_kernel,
                           (const void*)int8_split_kernel<16>, (const void*)int8_split_kernel<32>, (const void*)int8_split_kernel<64>, (const void*)int8_split_kernel<128>})
         if (e == cudaSuccess) e = allow_shared_memory(k);
-    if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
-    if (e == cudaSuccess) { *d.err = 0; e = cudaHostGetDevicePointer((void**)&d.err_dev, d.err, 0); }
+    if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, kErrWords * sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
+    if (e == cudaSuccess) { std::fill_n(d.err, kErrWords, 0u); e = cudaHostGetDevicePointer((void**)&d.err_dev, d.err, 0); }
     d.ready = e == cudaSuccess;
     return e;
 }
@@ -723,20 +730,11 @@ bool operand_map(CUtensorMap* m, const int8_t* q, int64_t rows, int64_t ld, int6
     return encode_tensor_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, q, 2, dims, strides, box, msg, msg_len, what);
 }
 
-int launch(const Int8Product& p, cudaStream_t s)
+int launch(const Int8Product& p, unsigned int* err, const Device* d, cudaStream_t s)
 {
     const auto cuda_fail = [](cudaError_t e) { cudaGetLastError(); return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", cudaGetErrorString(e)); };
-    int index = 0;
-    Device* d = nullptr;
-    cudaError_t e = cudaGetDevice(&index);
-    if (e == cudaSuccess) e = device_for(index, &d);
-    if (e != cudaSuccess) return cuda_fail(e);
-    if (const unsigned int code = p.err ? 0u : *(volatile unsigned int*)d->err) {
-        *(volatile unsigned int*)d->err = 0;
-        return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of an earlier product gave up (code %u); its result is not complete", code);
-    }
+    cudaError_t e;
     Out o = {p.y, p.ldy, p.y_type, 0, p.x_scale, p.w_scale, p.bias, p.relu ? 0.f : -INFINITY, 1.f, (int)p.M, (int)p.N};
-    unsigned int* const err = p.err ? p.err : d->err_dev;
     const int64_t size = p.y_type == ST_F32 ? 4 : 2;
     o.wide = aligned(p.y, 16) && (p.M == 1 || p.ldy * size % 16 == 0);
     const bool tma = aligned(p.x, 16) && aligned(p.w, 16) && (p.M == 1 || p.ldx % 16 == 0) && (p.N == 1 || p.ldw % 16 == 0);
@@ -869,7 +867,22 @@ int int8_matmul(const Int8Product& p, cudaStream_t s)
     if (p.bias) b.add("bias", p.bias, 4, N, false);
     b.add("y", p.y, p.y_type == ST_F32 ? 4 : 2, (M - 1) * p.ldy + N, true);
     if (!b.ok()) return b.status();
-    return launch(p, s);
+    const auto cuda_fail = [](cudaError_t e) { cudaGetLastError(); return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", cudaGetErrorString(e)); };
+    Device* d = nullptr;
+    int word = 0;
+    const cudaError_t e = device_for(b.device(), s, &d, &word);
+    if (e != cudaSuccess) return cuda_fail(e);
+    if (p.err) return launch(p, p.err, d, s);
+    // what an earlier product has left is told once, and this product is enqueued all the same: what gave up need not be the caller's
+    const unsigned int code = __atomic_exchange_n(d->err + word, 0u, __ATOMIC_RELAXED);
+    const int status = launch(p, d->err_dev + word, d, s);
+    if (status != ST_OK) {
+        unsigned int none = 0;
+        if (code) __atomic_compare_exchange_n(d->err + word, &none, code, false, __ATOMIC_RELAXED, __ATOMIC_RELAXED);
+        return status;
+    }
+    if (code) return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of an earlier product on this stream gave up (code %u); its result is not complete", code);
+    return ST_OK;
 }
 
 }  // namespace st

@@ -335,6 +335,27 @@ def test_a_wait_that_runs_out_is_reported(m, n, k, monkeypatch):
     assert torch.equal(y.cpu(), ref_matmul(x, sx, w, sw, None, False, "f32"))
 
 
+def test_a_product_that_gave_up_is_told_of_on_its_own_stream(monkeypatch):
+    """A call on another stream is neither refused nor told; the call on the same stream is told, and its own product is there."""
+    m, n, k = 300, 200, 1024
+    x, w, sx, sw = matrix(m, k, 0), matrix(n, k, 1), torch.rand(m, device="cuda"), torch.rand(n, device="cuda")
+    ys = [torch.zeros(m, n, device="cuda") for _ in range(3)]
+    other = torch.cuda.Stream()
+    st.st_int8_matmul(x, sx, w, sw, ys[0], cuda_stream=stream())
+    monkeypatch.setenv("ST_TEST_STALL_INT8", "1")
+    st.st_int8_matmul(x, sx, w, sw, ys[0], cuda_stream=stream())
+    monkeypatch.delenv("ST_TEST_STALL_INT8")
+    torch.cuda.synchronize()
+    st.st_int8_matmul(x, sx, w, sw, ys[1], cuda_stream=other.cuda_stream)
+    with pytest.raises(st.StError) as ei:
+        st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())
+    assert ei.value.status == st.ST_ERR_CUDA and "gave up" in str(ei.value)
+    torch.cuda.synchronize()
+    want = ref_matmul(x, sx, w, sw, None, False, "f32")
+    assert torch.equal(ys[1].cpu(), want) and torch.equal(ys[2].cpu(), want)
+    st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())
+
+
 # ---------------------------------------------------------------------------- with a context
 @pytest.mark.parametrize("h,w,k", [(10, 37, 96), (45, 80, 200)])
 def test_the_front_parts_last_layer_in_8_bits(h, w, k):
