@@ -819,10 +819,12 @@ const char* grad_fault(const st_adamw* o, int i, const void* grad)
     return nullptr;
 }
 
-st_status check_launch(st_adamw* o, const char* what)
+// From what the launches returned: the thread's last error may be an earlier call's, and a step that is reported as failed must not have been enqueued
+st_status check_launch(st_adamw* o, cudaError_t e, const char* what)
 {
-    cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? ST_OK : fail(o, ST_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    if (e == cudaSuccess) return ST_OK;
+    cudaGetLastError();
+    return fail(o, ST_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
 st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adamw* o)
@@ -932,7 +934,8 @@ st_status move_moments(st_adamw* o, const void* const* m, const void* const* v, 
             if (f) return fail(o, ST_ERR_INVALID_ARG, "%s: tensor %d: a buffer %s", what, i, f);
         }
     constexpr int group = kPointers / 2;
-    for (int first = 0; first < o->n; first += group) {
+    cudaError_t e = cudaSuccess;
+    for (int first = 0; first < o->n && e == cudaSuccess; first += group) {
         const int last = std::min(o->n, first + group);
         PointerArgs a;
         for (int i = first; i < last; ++i) { a.q[2 * (i - first)] = m ? m[i] : nullptr; a.q[2 * (i - first) + 1] = v ? v[i] : nullptr; }
@@ -940,9 +943,9 @@ st_status move_moments(st_adamw* o, const void* const* m, const void* const* v, 
         if (begin == end) continue;
         const int grid = (int)std::min<int64_t>(end - begin, std::max<int64_t>(o->moments_resident, (end - begin) / o->moments_span));
         auto kernel = write ? (o->bits == 32 ? adamw_write_kernel<32> : adamw_write_kernel<8>) : (o->bits == 32 ? adamw_read_kernel<32> : adamw_read_kernel<8>);
-        launch_early(pdl_enabled(), kernel, dim3(grid), dim3(kThreads), 0, o->stream, o->plan, first, begin, end, a);
+        e = launch_early(pdl_enabled(), kernel, dim3(grid), dim3(kThreads), 0, o->stream, o->plan, first, begin, end, a);
     }
-    return check_launch(o, what);
+    return check_launch(o, e, what);
 }
 
 }  // namespace
@@ -977,13 +980,14 @@ st_status st_adamw_set_grads(st_adamw* o, const void* const* grads)
     if (!guard.ok) return fail(o, ST_ERR_CUDA, "st_adamw_set_grads: cannot use the optimiser's device");
     for (int i = 0; i < o->n; ++i)
         if (const char* f = grad_fault(o, i, grads[i])) return fail(o, ST_ERR_INVALID_ARG, "st_adamw_set_grads: gradient %d %s", i, f);
-    for (int first = 0; first < o->n; first += kPointers) {
+    cudaError_t e = cudaSuccess;
+    for (int first = 0; first < o->n && e == cudaSuccess; first += kPointers) {
         const int count = std::min(kPointers, o->n - first);
         PointerArgs a;
         std::copy(grads + first, grads + first + count, a.q);
-        adamw_set_grads_kernel<<<(count + 127) / 128, 128, 0, o->stream>>>(o->plan.grads, first, count, a);
+        e = launch_early(false, adamw_set_grads_kernel, dim3((count + 127) / 128), dim3(128), 0, o->stream, o->plan.grads, first, count, a);
     }
-    return check_launch(o, "st_adamw_set_grads");
+    return check_launch(o, e, "st_adamw_set_grads");
 }
 
 st_status st_adamw_set_lr(st_adamw* o, double lr)
@@ -992,8 +996,7 @@ st_status st_adamw_set_lr(st_adamw* o, double lr)
     if (!(lr >= 0 && lr <= FLT_MAX)) return fail(o, ST_ERR_INVALID_ARG, "st_adamw_set_lr: lr must be >= 0 and finite in fp32");
     OnDevice guard(o->device);
     if (!guard.ok) return fail(o, ST_ERR_CUDA, "st_adamw_set_lr: cannot use the optimiser's device");
-    adamw_set_lr_kernel<<<1, 1, 0, o->stream>>>(o->plan.sc, (float)lr);
-    return check_launch(o, "st_adamw_set_lr");
+    return check_launch(o, launch_early(false, adamw_set_lr_kernel, dim3(1), dim3(1), 0, o->stream, o->plan.sc, (float)lr), "st_adamw_set_lr");
 }
 
 st_status st_adamw_step(st_adamw* o, float grad_scale, float* norm_out)
@@ -1008,10 +1011,12 @@ st_status st_adamw_step(st_adamw* o, float grad_scale, float* norm_out)
         if (f) return fail(o, ST_ERR_INVALID_ARG, "st_adamw_step: norm_out %s", f);
     }
     const int with_norm = o->always_norm || norm_out;
-    if (with_norm) launch_early(pdl_enabled(), adamw_norm_kernel, dim3(o->norm_grid), dim3(kThreads), 0, o->stream, o->plan, grad_scale, norm_out);
-    launch_early(pdl_enabled(), o->bits == 32 ? adamw_step_kernel<32> : adamw_step_kernel<8>, dim3(o->step_grid), dim3(kThreads), 0, o->stream,
-                 o->plan, grad_scale, with_norm);
-    return check_launch(o, "st_adamw_step");
+    cudaError_t e = cudaSuccess;
+    if (with_norm) e = launch_early(pdl_enabled(), adamw_norm_kernel, dim3(o->norm_grid), dim3(kThreads), 0, o->stream, o->plan, grad_scale, norm_out);
+    // no step without the norm that it was to be clipped by
+    if (e == cudaSuccess) e = launch_early(pdl_enabled(), o->bits == 32 ? adamw_step_kernel<32> : adamw_step_kernel<8>, dim3(o->step_grid), dim3(kThreads), 0, o->stream,
+                                           o->plan, grad_scale, with_norm);
+    return check_launch(o, e, "st_adamw_step");
 }
 
 st_status st_adamw_read_moments(st_adamw* o, float* const* m, float* const* v)

@@ -445,10 +445,10 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
             const unsigned grid = (unsigned)(groups * ((cols + kSlab - 1) / kSlab));
             cudaError_t e = cudaMemsetAsync(scale, 0, sizeof(float) * rows, s);
             if (e != cudaSuccess) return e;
-            plane_tops_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, (uint32_t*)scale, groups);
-            plane_integers_kernel<T><<<grid, 32 * kPlaneWarps, 0, s>>>(x, rows, n, rs, cs, q, ldq, (const uint32_t*)scale, groups);
-            plane_scales_kernel<<<(unsigned)((rows + 255) / 256), 256, 0, s>>>(scale, rows);
-            return cudaGetLastError();
+            e = launch_early(false, plane_tops_kernel<T>, dim3(grid), dim3(32 * kPlaneWarps), 0, s, x, rows, n, rs, cs, (uint32_t*)scale, groups);
+            if (e == cudaSuccess) e = launch_early(false, plane_integers_kernel<T>, dim3(grid), dim3(32 * kPlaneWarps), 0, s, x, rows, n, rs, cs, q, ldq, (const uint32_t*)scale, groups);
+            if (e == cudaSuccess) e = launch_early(false, plane_scales_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, s, scale, rows);
+            return e;
         }
         const auto go = [&](auto kernel, const T* from, int64_t first, int64_t count) {
             return launch_early(early, kernel, dim3((unsigned)((count + per - 1) / per)), dim3(32 * kPlaneWarps), 0, s, from, count, n, rs, cs, q + first * ldq, ldq, scale + first, words);
@@ -507,7 +507,6 @@ extern "C" st_status st_quantize_rows(const void* x, int32_t x_type, int64_t row
     cudaError_t e = x_type == ST_F32 ? launch((const float*)x, rows, cols, row_stride, col_stride, q, ldq, scale, s)
                   : x_type == ST_BF16 ? launch((const bf16*)x, rows, cols, row_stride, col_stride, q, ldq, scale, s)
                                       : launch((const __half*)x, rows, cols, row_stride, col_stride, q, ldq, scale, s);
-    if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) { cudaGetLastError(); return (st_status)fail_on_thread(ST_ERR_CUDA, "st_quantize_rows: %s", cudaGetErrorString(e)); }
     return ST_OK;
 }

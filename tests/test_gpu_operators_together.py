@@ -107,3 +107,37 @@ def test_the_contexts_adam_and_st_adamw_take_the_same_steps(side_stream):
     assert st.st_adamw_step_count(opt) == 5
     st.st_adamw_destroy(opt)
     st.st_destroy(ctx)
+
+
+def test_an_error_of_an_earlier_call_is_not_the_operators(side_stream):
+    """A step that finds no memory for its confusion matrices leaves the runtime's last error behind.  What is enqueued after that succeeds and says so:
+    a caller that is told otherwise would step twice."""
+    stream = side_stream.cuda_stream
+    S, C = 8000, 255                                    # 64 matrices a stream: 266 GB, one request that cannot be met
+    ctx = st.st_init_head(n_streams=S, c_in=1, n_classes=C, feat_h=1, feat_w=1, cuda_stream=stream, init_params=np.zeros(S * 2 * C, np.float32))
+    feature, label = torch.zeros(1, device="cuda"), torch.zeros(16, dtype=torch.uint8, device="cuda")
+    for i in range(S):
+        st.st_set_frozen_features(ctx, i, feature)
+        st.st_set_labels(ctx, i, label)
+    conf = np.empty((S, 1, C, C), np.int64)             # never touched
+
+    def fails_for_want_of_memory():
+        with pytest.raises(st.StError) as ei:
+            st.st_distill_step(ctx, 1, None, conf)
+        assert ei.value.status == st.ST_ERR_OOM
+
+    p, m, v, g = put(np.ones(1000), "f32"), torch.zeros(1000, device="cuda"), torch.zeros(1000, device="cuda"), put(np.ones(1000), "f32")
+    opt = st.st_adamw_create([p], [m], [v], [g], lr=0.1, max_norm=1.0, cuda_stream=stream)
+    out = torch.zeros(1000, device="cuda")
+    x = torch.randn(300, 20, device="cuda")
+    planes = torch.randn(700, 20, device="cuda")
+    q, s = torch.zeros(20, 704, dtype=torch.int8, device="cuda")[:, :700], torch.zeros(300, device="cuda")
+    for call in (lambda: st.st_adamw_step(opt), lambda: st.st_adamw_set_grads(opt, [g]), lambda: st.st_adamw_set_lr(opt, 0.2),
+                 lambda: st.st_adamw_read_moments(opt, [out]), lambda: st.st_adamw_write_moments(opt, [out]),
+                 lambda: st.st_quantize_rows(x, torch.zeros(300, 32, dtype=torch.int8, device="cuda")[:, :20], s, cuda_stream=stream),
+                 lambda: st.st_quantize_rows(planes.t(), q, s, cuda_stream=stream)):
+        fails_for_want_of_memory()
+        call()
+    assert st.st_adamw_step_count(opt) == 1
+    st.st_adamw_destroy(opt)
+    st.st_destroy(ctx)
