@@ -181,10 +181,12 @@ __device__ __forceinline__ void decode(float (&m)[kPer], float (&root)[kPer], co
     }
 }
 
-// The level floor(sqrt(r) + 1/2).  The approximate root lies within 2^-23 of the root, and so does that of a ratio formed from an approximate root
-// (half of 2^-23 and 2^-24 more).  So rounding it to the nearest whole number gives the level unless it lies next to a border: within
-// 127 * 2^-23 = 1.6e-5 of one for m, 255 * 1.75 * 2^-23 = 5.4e-5 for sqrt(v).  There the border, which fp32 holds exactly, decides.
-constexpr float kNearM = 2e-5f, kNearV = 6e-5f, kRound = 12582912.f;        // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
+// The level floor(sqrt(r) + 1/2).  The approximate root lies within 2^-23 of the root.  The ratio of sqrt(v) is formed from an approximate root (2^-23 of
+// itself) and rounded, the one that defines the level from the rounded root (2^-24) and rounded too: 2.5 * 2^-23 between the two, half of it between
+// their roots.  So rounding the approximate root to the nearest whole number gives the level unless it lies next to a border: within 127 * 2^-23 = 1.6e-5
+// of one for m, 255 * 2.25 * 2^-23 = 6.9e-5 for sqrt(v).  There the border, which fp32 holds exactly, decides.
+constexpr float kNearM = 2e-5f, kNearV = 7.5e-5f, kRound = 12582912.f;      // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
+static_assert(kNearM > 127 * 0x1p-23 && kNearV > 255 * 2.25 * 0x1p-23, "values next to a border would not be looked at exactly");
 __device__ __forceinline__ float approximate_root(float r)
 {
     float s;
@@ -377,7 +379,7 @@ __device__ __forceinline__ void fetch_8(Loads8& l, const TensorRec& t, const voi
     else fetch<true>(l.p, t.param, PARAM, at, kBlockVals, lane);
 }
 // A lane's codes of a block, exactly, from what the block's step reads (old codes and scales, which must not have been overwritten) and the
-// reciprocals of its new scales.  Out of line: a lane in 800 comes here, and its registers are not the step's.
+// reciprocals of its new scales.  Out of line: a lane in 660 comes here, and its registers are not the step's.
 template <int GRAD>
 __device__ __noinline__ uint4 exact_codes(const TensorRec* t, const void* grad, StepNow k, int64_t at, float im, float iv)
 {

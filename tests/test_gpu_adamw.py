@@ -294,6 +294,28 @@ def test_moments_that_fade_away_end_at_zero():
     assert torch.isfinite(params[0]).all()
 
 
+@pytest.mark.parametrize("shift", [0, 1])
+def test_levels_next_to_their_borders(shift):
+    """Second moments whose root lies on a border between two of the upper levels, or up to four steps of fp32 beside it: the levels are those that the
+    fp32 operations of the definition give, by the path of whole vectors and by that of single values."""
+    f, blocks, b2 = np.float32, 2000, 0.5               # 1 - b2 is exact, and so is its product
+    rng = np.random.default_rng(11)
+    g = np.empty((blocks, BLOCK), f)
+    g[:, 0] = rng.uniform(0.5, 2, blocks).astype(f)
+    top = np.sqrt((g[:, 0] * g[:, 0]) * f(1 - b2))      # the block's largest root, and the scale of the step
+    scale = (top / f(255 * 255)).astype(f)
+    level = rng.integers(150, 254, (blocks, BLOCK - 1)) + 0.5
+    root = level ** 2 * scale.astype(np.float64)[:, None]
+    near = (root / np.sqrt(1 - b2)).astype(f).view(np.int32) + rng.integers(-4, 5, root.shape)
+    g[:, 1:] = near.astype(np.int32).view(f)
+    made = make([g.size], 8, shift=shift, b1=0.0, b2=b2, wd=0.0)
+    made[6][0].copy_(torch.from_numpy(g.reshape(-1)).cuda())
+    made[7][0].step(g.reshape(-1).astype(np.float64))
+    st.st_adamw_step(made[0])
+    assert np.array_equal(made[4][0].cpu().numpy(), made[7][0].cv) and np.array_equal(made[3][0].cpu().numpy(), made[7][0].cm)
+    assert np.array_equal(made[5][1][0].cpu().numpy(), made[7][0].vs)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_moments_go_out_and_come_back(bits):
     sizes = [5, 1000, 256, 3]
