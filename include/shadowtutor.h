@@ -363,7 +363,7 @@ typedef enum st_dtype { ST_F32 = 0, ST_BF16 = 1, ST_F16 = 2 } st_dtype;
  *     p <- p - lr wd p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * lr and wd of a tensor are the optimiser's lr times the tensor's lr_scale, and the tensor's weight_decay.  f is grad_scale of the
  * call, times min(1, max_norm / (norm + 1e-6)) with max_norm > 0; norm is the Euclidean norm of all gradients together, grad_scale
- * included, summed in double in an order that depends on the tensors' sizes alone.
+ * included, summed in double in an order that depends on the tensors' sizes and the device alone: not on where the gradients lie.
  *
  * Moments in 32 bits are fp32 [n] each.  Moments in 8 bits are one byte a value, in blocks of ST_ADAMW_BLOCK consecutive values of a
  * tensor (its last block may be shorter) with one fp32 scale each:

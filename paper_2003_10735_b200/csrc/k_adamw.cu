@@ -7,7 +7,8 @@
 // load to the store, so that every buffer is read once and written once.
 //
 // The gradients' norm needs every gradient before the first step is taken: a kernel of its own (double accumulators, partial
-// sums per block added in block order: the result depends on nothing but the values and the launch).
+// sums per block added in block order, a lane's values in theirs wherever the gradients lie: the result depends on the values, the tensors' sizes and
+// the number of blocks that the device holds).
 #include "../../include/shadowtutor.h"
 #include "st_internal.h"
 
@@ -584,14 +585,24 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
 {
     __shared__ double shared[kWarps];
     __shared__ bool last;
+    __shared__ __align__(16) float turned[kWarps][kBlockVals];
     Share share = share_of(p, 0, p.n_chunks, blockIdx.x, gridDim.x);
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     double sum = 0;
+    // Values that were loaded one by one are handed on so that each lane adds the eight that it has on the vector path
     const auto add = [&](const Raw& r, int type, auto vec) {
         float g[kPer];
         convert<decltype(vec)::value>(g, r, type);
+        if (!decltype(vec)::value) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) turned[warp][32 * j + lane] = g[j];
+            __syncwarp();
+            const float4 a = *(const float4*)&turned[warp][kPer * lane], b = *(const float4*)&turned[warp][kPer * lane + 4];
+            g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+        }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) { const double d = g[j]; sum = fma(d, d, sum); }
     };

@@ -412,6 +412,24 @@ def test_the_norm_is_the_same_every_time():
     assert len(seen) == 1
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_the_norm_does_not_depend_on_where_gradients_lie(kind):
+    """The sum of squares is (1 + 2^-24)^2, whose root lies between two fp32 numbers, and four squares that double loses or keeps, depending on what they are added to."""
+    u, tiny = 2.0 ** -12, 1.25 * 2.0 ** -27
+    up = 1.0 if kind != "f16" else 2.0 ** 14            # fp16 holds nothing below 2^-24
+    g = np.zeros(700)
+    g[256:264] = np.array([1, u, tiny, tiny, 2.0 ** -24, u, tiny, tiny]) * up
+    seen = set()
+    for shift in (0, 1, 2, 3, 4, 8):
+        made = make([700], 32, grad=kind, shift=shift)
+        made[6][0].copy_(torch.from_numpy(g).to(TYPES[kind]).cuda())
+        assert np.array_equal(f64(made[6][0]), g)       # the type holds them
+        norm = torch.zeros(1, device="cuda")
+        st.st_adamw_step(made[0], norm_out=norm)
+        seen.add(norm.item())
+    assert len(seen) == 1, seen
+
+
 def test_norm_of_gradients_whose_squares_leave_fp32():
     made = make([64, 64], 32)
     made[6][0].fill_(1e25)
