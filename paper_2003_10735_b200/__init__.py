@@ -489,12 +489,25 @@ def st_set_frozen_features_int8(ctx: _Ctx, stream: int, x, x_scale, w, w_scale, 
 class _AdamW:
     """Handle of an st_adamw, with the tensors that it works on (they must outlive it)."""
 
-    def __init__(self, handle, sizes, grad_names, keep):
+    def __init__(self, handle, sizes, grad_names, keep, cuda_stream):
         self.handle = handle
         self.sizes = sizes
         self.grad_names = grad_names
         self.keep = keep
-        self.grads = None
+        self.cuda_stream = cuda_stream
+        self.grads = []
+
+    def let_go(self, grads) -> None:
+        """Hold other gradients than so far.  Steps that are enqueued may still read those: where the optimiser works on another stream than the caller,
+        their memory is not used again before.  (0.8 us a tensor, which callers on the optimiser's stream do not pay: there, memory is used again in order.)"""
+        gone = [old for old, new in zip(self.grads, grads) if old is not None and old is not new]
+        if gone:
+            import torch
+            if torch.cuda.current_stream(gone[0].device).cuda_stream != self.cuda_stream:
+                stream = torch.cuda.ExternalStream(self.cuda_stream, device=gone[0].device)
+                for old in gone:
+                    old.record_stream(stream)
+        self.grads = grads
 
     def __del__(self):
         try:
@@ -577,16 +590,18 @@ def st_adamw_create(params, exp_avg, exp_avg_sq, grads=None, exp_avg_scale=None,
     desc = st_adamw_desc(count, 8 if eight else 32, lr, beta1, beta2, eps, max_norm, int(skip_nonfinite), first_step, cuda_stream or None)
     out = ctypes.c_void_p()
     _check_adamw(load_library().st_adamw_create(ctypes.byref(desc), table, ctypes.byref(out)), None)
-    opt = _AdamW(out.value, sizes, grad_names, (list(params), list(exp_avg), list(exp_avg_sq), scales, list(masters)))
-    opt.grads = list(grads)
+    opt = _AdamW(out.value, sizes, grad_names, (list(params), list(exp_avg), list(exp_avg_sq), scales, list(masters)), cuda_stream or 0)
+    opt.let_go(list(grads))
     return opt
 
 
 def st_adamw_set_grads(opt: _AdamW, grads) -> None:
-    """Where the gradients are from now on (None: leave that tensor alone); the tensors must outlive the steps that read them."""
+    """Where the gradients are from now on (None: leave that tensor alone).  The optimiser holds them until others are given, and tells torch's
+    allocator where its stream has used those of the current stream; what writes them has to be waited for by that stream, as always.  Tensors that a
+    replayed graph reads must outlive the replays."""
     table = _pointers(grads, opt.sizes, opt.grad_names, "grads")
     _check_adamw(load_library().st_adamw_set_grads(opt.handle, _address(table)), opt)
-    opt.grads = list(grads)
+    opt.let_go(list(grads))
 
 
 def st_adamw_set_lr(opt: _AdamW, lr: float) -> None:

@@ -383,6 +383,30 @@ def test_negative_second_moments_are_taken_as_zero():
         assert (f64(out)[:5] == 0).all() and (f64(out)[5:] > 0).all()
 
 
+def test_gradients_that_are_replaced_stay_until_their_step_is_done(side_stream):
+    """The optimiser works on another stream than the one that gradients come from, and is behind: the memory of gradients that it was given before
+    does not go to tensors of the other stream meanwhile."""
+    n, own = 300_000, torch.cuda.Stream()
+    p, m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    before, after = torch.ones(n, device="cuda"), torch.full((n,), 1.0, device="cuda")
+    side_stream.synchronize()
+    opt = st.st_adamw_create([p], [m], [v], [before], lr=0.1, weight_decay=0.0, cuda_stream=own.cuda_stream)
+    st.st_adamw_set_grads(opt, [before])
+    st.st_adamw_step(opt)                               # kernels are loaded before the wait
+    own.synchronize()
+    with torch.cuda.stream(own):
+        torch.cuda._sleep(200_000_000)                  # a tenth of a second
+    st.st_adamw_step(opt)
+    st.st_adamw_set_grads(opt, [after])
+    del before
+    other = [torch.full((n,), float("nan"), device="cuda") for _ in range(4)]
+    side_stream.synchronize()
+    assert not own.query()                              # the step has not run yet
+    own.synchronize()
+    assert torch.isfinite(p).all() and len(other) == 4
+    st.st_adamw_destroy(opt)
+
+
 def test_more_tensors_than_one_launch_can_name():
     n = 1000
     sizes = [1 + i % 7 for i in range(n)]
