@@ -398,7 +398,7 @@ typedef struct st_adamw_desc {
     int32_t state_bits;        /* 32 or 8 */
     double lr;                 /* >= 0 */
     double beta1, beta2;       /* in [0, 1) */
-    double eps;                /* at least FLT_MIN */
+    double eps;                /* FLT_MIN .. 2^100 */
     double max_norm;           /* 0: gradients are not clipped */
     int32_t skip_nonfinite;    /* 1: where the gradients' norm is not finite nothing is changed and the step is not counted */
     int64_t first_step;        /* steps taken before (a resumed training); 0 at the beginning */

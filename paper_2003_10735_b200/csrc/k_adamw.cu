@@ -283,6 +283,9 @@ __device__ __forceinline__ float root_of(float v)
     return v == 0.f ? 0.f : small ? r * 0x1p-48f : r;
 }
 __device__ __forceinline__ float approximate_reciprocal(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// Below kMostEps a denominator above 2^125, whose reciprocal leaves fp32's normal range, has a root that has left fp32: finite roots end at 1.9e19, times
+// r2 of 9.5e7 at most (the largest beta2 below 1).
+constexpr double kMostEps = 0x1p100;
 __device__ __forceinline__ float quotient(float m, float den)       // den >= FLT_MIN, or NaN
 {
     const float y = approximate_reciprocal(den), q = m * y;
@@ -972,8 +975,8 @@ st_status st_adamw_create(const st_adamw_desc* desc, const st_adamw_tensor* tens
     const st_adamw_desc& d = *desc;
     if (d.n_tensors < 1 || d.n_tensors > 65535) return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: n_tensors %d outside 1..65535", d.n_tensors);
     if (d.state_bits != 32 && d.state_bits != 8) return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: state_bits must be 32 or 8");
-    if (!(d.lr >= 0 && d.lr <= FLT_MAX) || !(d.beta1 >= 0 && d.beta1 < 1) || !(d.beta2 >= 0 && d.beta2 < 1) || !(d.eps >= FLT_MIN && d.eps <= FLT_MAX))
-        return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: needs lr >= 0, beta1 and beta2 in [0, 1) and eps >= %g", (double)FLT_MIN);
+    if (!(d.lr >= 0 && d.lr <= FLT_MAX) || !(d.beta1 >= 0 && d.beta1 < 1) || !(d.beta2 >= 0 && d.beta2 < 1) || !(d.eps >= FLT_MIN && d.eps <= kMostEps))
+        return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: needs lr >= 0, beta1 and beta2 in [0, 1) and eps in %g..%g", (double)FLT_MIN, kMostEps);
     if (!(d.max_norm >= 0) || !std::isfinite(d.max_norm) || d.first_step < 0 || (d.skip_nonfinite & ~1))
         return (st_status)fail_on_thread(ST_ERR_INVALID_ARG, "st_adamw_create: needs max_norm >= 0, first_step >= 0 and skip_nonfinite 0 or 1");
     st_adamw* o = new (std::nothrow) st_adamw;

@@ -34,6 +34,15 @@ def test_create_refuses_descriptions(lib, kw):
     assert "st_adamw_create" in st.st_adamw_last_error(None) and st.st_adamw_last_error(None) == st.st_last_error(None)
 
 
+@pytest.mark.parametrize("eps,refused", [(2.0 ** 100, False), (2.0 ** 101, True), (5e37, True), (3.4e38, True)])
+def test_an_eps_that_leaves_no_room_for_the_root_is_refused(lib, eps, refused):
+    """Denominators above 2^125 are those of roots that have left fp32; an eps of that size would be taken for one."""
+    empty = (st.st_adamw_tensor * 1)(st.st_adamw_tensor(param_type=7))         # refused for its type where eps is not
+    status, handle = _create(lib, empty, eps=eps)
+    assert status != st.ST_OK and handle is None
+    assert ("needs lr" in st.st_adamw_last_error(None)) == refused
+
+
 def test_null_arguments(lib):
     out = ctypes.c_void_p()
     assert lib.st_adamw_create(None, None, ctypes.byref(out)) == st.ST_ERR_INVALID_ARG
