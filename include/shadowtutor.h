@@ -440,7 +440,7 @@ ST_API st_status st_adamw_step(st_adamw *opt, float grad_scale, float *norm_out)
  * st_adamw_read_moments / st_adamw_write_moments — the moments as fp32 values, whatever they are held in: what a checkpoint keeps, and
  * how it moves between 8 and 32 bits.  Work is enqueued on the optimiser's stream.
  *   exp_avg, exp_avg_sq   host arrays of n_tensors device pointers to fp32 [n] each; a NULL entry leaves that tensor's moment out, a
- *                         NULL array all of them.  Reading: the buffers must not overlap the optimiser's own.
+ *                         NULL array all of them.  Reading: the buffers must not overlap one another or the optimiser's own.
  * Written into 8 bits, values are rounded to levels as a step does.  Negative second moments are taken as 0.
  */
 ST_API st_status st_adamw_read_moments(st_adamw *opt, float *const *exp_avg, float *const *exp_avg_sq);

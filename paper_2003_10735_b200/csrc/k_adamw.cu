@@ -826,6 +826,15 @@ bool touches(const std::vector<st_adamw::Range>& sorted, uintptr_t begin, uintpt
     return it != sorted.end() && it->begin < end;
 }
 
+// Sorts them
+bool overlap(std::vector<st_adamw::Range>& ranges)
+{
+    std::sort(ranges.begin(), ranges.end(), [](const st_adamw::Range& a, const st_adamw::Range& b) { return a.begin < b.begin; });
+    for (size_t i = 1; i < ranges.size(); ++i)
+        if (ranges[i].begin < ranges[i - 1].end) return true;
+    return false;
+}
+
 const char* grad_fault(const st_adamw* o, int i, const void* grad)
 {
     if (!grad || o->values[i] == 0) return nullptr;
@@ -878,9 +887,7 @@ st_status create(const st_adamw_desc& d, const st_adamw_tensor* tensors, st_adam
         }
         r.vec = aligned(t.param, kPer * type_size(t.param_type)) && aligned(t.master, kPer * 4) && aligned(t.exp_avg, kPer * moment) && aligned(t.exp_avg_sq, kPer * moment);
     }
-    std::sort(o->written.begin(), o->written.end(), [](const st_adamw::Range& a, const st_adamw::Range& b) { return a.begin < b.begin; });
-    for (size_t i = 1; i < o->written.size(); ++i)
-        if (o->written[i].begin < o->written[i - 1].end) return fail(nullptr, ST_ERR_INVALID_ARG, "st_adamw_create: two buffers that a step writes overlap");
+    if (overlap(o->written)) return fail(nullptr, ST_ERR_INVALID_ARG, "st_adamw_create: two buffers that a step writes overlap");
     for (int i = 0; i < d.n_tensors; ++i)
         if (const char* f = grad_fault(o, i, tensors[i].grad)) return fail(nullptr, ST_ERR_INVALID_ARG, "st_adamw_create: tensor %d: grad %s", i, f);
 
@@ -942,13 +949,16 @@ st_status move_moments(st_adamw* o, const void* const* m, const void* const* v, 
 {
     OnDevice guard(o->device);
     if (!guard.ok) return fail(o, ST_ERR_CUDA, "%s: cannot use the optimiser's device", what);
+    std::vector<st_adamw::Range> to;
     for (int i = 0; i < o->n; ++i)
         for (const void* q : {m ? m[i] : nullptr, v ? v[i] : nullptr}) {
             if (!q || o->values[i] == 0) continue;
+            if (!write) to.push_back({(uintptr_t)q, (uintptr_t)q + 4 * o->values[i]});
             const char* f = buffer_fault(q, 4, o->device);
             if (!f && touches(o->written, (uintptr_t)q, (uintptr_t)q + 4 * o->values[i])) f = "overlaps a buffer of the optimiser";
             if (f) return fail(o, ST_ERR_INVALID_ARG, "%s: tensor %d: a buffer %s", what, i, f);
         }
+    if (overlap(to)) return fail(o, ST_ERR_INVALID_ARG, "%s: two buffers that are written overlap", what);
     constexpr int group = kPointers / 2;
     cudaError_t e = cudaSuccess;
     for (int first = 0; first < o->n && e == cudaSuccess; first += group) {
@@ -1038,7 +1048,8 @@ st_status st_adamw_step(st_adamw* o, float grad_scale, float* norm_out)
 st_status st_adamw_read_moments(st_adamw* o, float* const* m, float* const* v)
 {
     if (!o) return ST_ERR_INVALID_ARG;
-    return move_moments(o, (const void* const*)m, (const void* const*)v, false, "st_adamw_read_moments");
+    try { return move_moments(o, (const void* const*)m, (const void* const*)v, false, "st_adamw_read_moments"); }
+    catch (const std::exception&) { return fail(o, ST_ERR_OOM, "st_adamw_read_moments: host allocation failed"); }
 }
 
 st_status st_adamw_write_moments(st_adamw* o, const float* const* m, const float* const* v)

@@ -347,6 +347,19 @@ def test_moments_go_out_and_come_back(bits):
     assert all(torch.equal(a, b) for a, b in zip(before[0], other[4])) and torch.equal(before[1], other[3][2])
 
 
+def test_reading_two_moments_into_the_same_place_is_refused():
+    opt = make([300, 40], 32)[0]
+    out = [torch.full((n,), 7.0, device="cuda") for n in (300, 40, 300, 40)]
+    for m, v in ((out[:2], [out[0], out[3]]), ([out[0], out[0][260:]], out[2:]), ([out[0], out[0][:40]], None)):
+        with pytest.raises(st.StError) as ei:
+            st.st_adamw_read_moments(opt, m, v)
+        assert ei.value.status == st.ST_ERR_INVALID_ARG and "overlap" in str(ei.value)
+    assert all((o == 7).all() for o in out)
+    st.st_adamw_write_moments(opt, [out[0], out[1]], [out[0], out[1]])          # what is only read may be the same
+    st.st_adamw_read_moments(opt, [out[0], out[1]], [out[2], out[3]])
+    assert all((o == 7).all() for o in out)
+
+
 def test_values_at_the_ends_of_the_range_step_like_others():
     """Moments that are 0, subnormal or near fp32's end, in one warp with ordinary ones."""
     vals = np.array([0.0, 1e-45, 1e-40, 1.2e-38, 1e-37, 1e-31, 1e-30, 1e-20, 1e-8, 1.0, 1e10, 1e30, 3e38])
