@@ -467,6 +467,7 @@ ST_API const char *st_adamw_last_error(const st_adamw *opt);
  *   rows, cols  rows >= 0, cols >= 1, at most 2^31 - 1 each (ST_ERR_UNSUPPORTED above).
  * Returns after enqueueing on cuda_stream (NULL = default stream), allocates nothing, and may be captured into a graph.
  * ST_ERR_INVALID_ARG: a pointer that is not memory of the current device, unaligned to its element or overlapping q or scale; bad extents.
+ * (Matrices of one pitch whose rows lie beside each other in one buffer do not overlap.)
  */
 ST_API st_status st_quantize_rows(const void *x, int32_t x_type, int64_t rows, int64_t cols, int64_t row_stride,
                                   int64_t col_stride, int8_t *q, int64_t ldq, float *scale, void *cuda_stream);

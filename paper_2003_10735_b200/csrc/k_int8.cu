@@ -860,12 +860,12 @@ int int8_matmul(const Int8Product& p, cudaStream_t s)
         return fail_on_thread(ST_ERR_UNSUPPORTED, "st_int8_matmul: extents beyond the kernels' 32-bit counts of tiles");
     if (M == 0 || N == 0) return ST_OK;
     Int8Buffers b("st_int8_matmul");
-    b.add("x", p.x, 1, (M - 1) * p.ldx + K, false);
+    b.add("x", p.x, 1, M, K, p.ldx, false);
     b.add("x_scale", p.x_scale, 4, M, false);
-    b.add("w", p.w, 1, (N - 1) * p.ldw + K, false);
+    b.add("w", p.w, 1, N, K, p.ldw, false);
     b.add("w_scale", p.w_scale, 4, N, false);
     if (p.bias) b.add("bias", p.bias, 4, N, false);
-    b.add("y", p.y, p.y_type == ST_F32 ? 4 : 2, (M - 1) * p.ldy + N, true);
+    b.add("y", p.y, p.y_type == ST_F32 ? 4 : 2, M, N, p.ldy, true);
     if (!b.ok()) return b.status();
     const auto cuda_fail = [](cudaError_t e) { cudaGetLastError(); return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: %s", cudaGetErrorString(e)); };
     Device* d = nullptr;

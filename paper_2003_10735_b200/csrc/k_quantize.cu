@@ -499,8 +499,10 @@ extern "C" st_status st_quantize_rows(const void* x, int32_t x_type, int64_t row
     if (rows == 0) return ST_OK;
     const int64_t size = x_type == ST_F32 ? 4 : 2;
     Int8Buffers b("st_quantize_rows");
-    b.add("x", x, size, (rows - 1) * row_stride + (cols - 1) * col_stride + 1, false);
-    b.add("q", q, 1, (rows - 1) * ldq + cols, true);
+    if (col_stride == 1 || cols == 1) b.add("x", x, size, rows, cols, row_stride, false);
+    else if (row_stride == 1 || rows == 1) b.add("x", x, size, cols, rows, col_stride, false);
+    else b.add("x", x, size, (rows - 1) * row_stride + (cols - 1) * col_stride + 1, false);
+    b.add("q", q, 1, rows, cols, ldq, true);
     b.add("scale", scale, 4, rows, true);
     if (!b.ok()) return b.status();
     cudaStream_t s = (cudaStream_t)cuda_stream;

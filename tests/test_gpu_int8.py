@@ -356,6 +356,37 @@ def test_a_product_that_gave_up_is_told_of_on_its_own_stream(monkeypatch):
     st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())
 
 
+@pytest.mark.parametrize("k,n", [(96, 48), (97, 33)])
+def test_matrices_that_lie_beside_each_other_in_one_buffer(k, n):
+    """Integers behind the rows that they are made from, products behind the integers: no byte is shared, and nothing else changes."""
+    m, pitch = 150, 1024
+    g = torch.Generator(device="cuda").manual_seed(k)
+    buf = torch.randint(0, 256, (m + 1, pitch), dtype=torch.uint8, generator=g, device="cuda")[:m]
+    x = buf[:, :4 * k].view(torch.float32)
+    x.copy_(torch.randn(m, k, generator=g, device="cuda"))
+    q = buf[:, 4 * k:5 * k].view(torch.int8)
+    y0 = -(-5 * k // 4) * 4
+    y = buf[:, y0:y0 + 4 * n].view(torch.float32)
+    scale, w, sw = torch.zeros(m, device="cuda"), matrix(n, k, 3), torch.rand(n, device="cuda")
+    before = buf.clone()
+    st.st_quantize_rows(x, q, scale, cuda_stream=stream())
+    want_q, want_s = ref_quantize(x.double().cpu().numpy())
+    assert np.array_equal(q.cpu().numpy(), want_q) and np.array_equal(scale.cpu().numpy(), want_s)
+    st.st_int8_matmul(q, scale, w, sw, y, cuda_stream=stream())
+    assert torch.equal(y.cpu(), ref_matmul(q, scale, w, sw, None, False, "f32"))
+    before[:, 4 * k:5 * k], before[:, y0:y0 + 4 * n] = buf[:, 4 * k:5 * k], buf[:, y0:y0 + 4 * n]
+    assert torch.equal(buf, before)
+    planes = torch.zeros(60, 256, device="cuda")                    # pixels of planes, integers behind each plane
+    st.st_quantize_rows(planes[:, :50].t(), planes.view(torch.int8)[:50, 400:460], torch.zeros(50, device="cuda"), cuda_stream=stream())
+    for call in (lambda: st.st_quantize_rows(x, buf[:, 4 * k - 1:5 * k - 1].view(torch.int8), scale),                      # a byte shared
+                 lambda: st.st_quantize_rows(x, buf[:, pitch - 1:].view(torch.int8).as_strided((m, k), (pitch, 1)), scale),          # in the next row
+                 lambda: st.st_int8_matmul(q, scale, w, sw, buf.view(torch.float32).as_strided((m, n), (pitch // 4 + 1, 1), y0 // 4)),     # another pitch
+                 lambda: st.st_int8_matmul(q, scale, w, sw, y, bias=y[3])):
+        with pytest.raises(st.StError) as ei:
+            call()
+        assert ei.value.status == st.ST_ERR_INVALID_ARG and "overlap" in str(ei.value)
+
+
 # ---------------------------------------------------------------------------- with a context
 @pytest.mark.parametrize("h,w,k", [(10, 37, 96), (45, 80, 200)])
 def test_the_front_parts_last_layer_in_8_bits(h, w, k):
