@@ -374,6 +374,13 @@ typedef enum st_dtype { ST_F32 = 0, ST_BF16 = 1, ST_F16 = 2 } st_dtype;
  * value and that value itself they are 1.6 to 16 per cent apart (m; v about half of that in its root).  The step works with the moments in fp32
  * (with 8 bits: each product and sum rounded by itself, so that equal inputs give equal levels) and parameters see them before they
  * are rounded to levels.  A block that holds a moment that is not finite decodes to values that are not finite or NaN.
+ * Levels are rounded to the nearest one after each step, so a moment that changes by less than half the distance of two levels in a step stays where it
+ * is.  m forgets a tenth a step (beta1 0.9) and does not come near that: it is 2 per cent off (root of the mean square).  v does with a beta2 near 1:
+ *     beta2 up to 0.99    99 of 100 sqrt(v) are within 5 per cent of what fp32 moments hold, however long the run
+ *     beta2 0.995         within 7 per cent; twice too large for a thousand steps where a value's gradients shrink tenfold and its block's largest do not
+ *     beta2 0.999         after 3,000 / 10,000 / 20,000 steps of gradients of one spread 1.06 / 1.2 / 1.35 times too large in the median, up to 1.45; where a
+ *                         value's gradients shrink tenfold and its block's largest do not, 3 times after 2,000 steps and 11 times after 5,000: it never shrinks with them
+ * Steps are too short by the same factors.  Training of more than some hundred steps with a beta2 above 0.99 takes 32-bit moments.
  */
 #define ST_ADAMW_BLOCK 256
 typedef struct st_adamw st_adamw; /* opaque, library-owned */

@@ -558,7 +558,9 @@ def st_adamw_create(params, exp_avg, exp_avg_sq, grads=None, exp_avg_scale=None,
     """Lists of CUDA tensors, one entry per parameter tensor.  `params` float32, bfloat16 or float16; `exp_avg` and `exp_avg_sq`
     float32, or int8 and uint8 with `exp_avg_scale` and `exp_avg_sq_scale` (float32, one value per ST_ADAMW_BLOCK values);
     `grads` and `masters` may hold None.  `weight_decay` and `lr_scale`: a number or one per tensor.  `grad_types`: names of the
-    gradients' types ("float32", "bfloat16", "float16"), one or one per tensor, where `grads` does not say (default: the parameter's)."""
+    gradients' types ("float32", "bfloat16", "float16"), one or one per tensor, where `grads` does not say (default: the parameter's).
+    8-bit second moments follow their recurrence for a `beta2` up to 0.99 only: the default's grow too large over thousands of steps (the header says
+    by how much), and with it 8-bit moments serve short fine-tuning.  Parameters change in place behind autograd's back, as their `.data` does."""
     count = len(params)
     sizes = [p.numel() for p in params]
     eight = count > 0 and str(exp_avg[0].dtype).removeprefix("torch.") == "int8"

@@ -294,6 +294,33 @@ def test_moments_that_fade_away_end_at_zero():
     assert torch.isfinite(params[0]).all()
 
 
+@pytest.mark.parametrize("b2,steady,shrunk", [(0.99, (0.95, 1.05), (0.93, 1.08)), (0.999, (1.0, 1.3), (2.0, 6.0))])
+def test_moments_in_8_bits_over_thousands_of_steps(b2, steady, shrunk):
+    """3,000 steps against the definition, level by level, and against fp32 moments.  After the first 1,000 the gradients of half of each block fall tenfold.
+    The ranges of the medians are those that the header gives: with beta2 0.99 sqrt(v) follows, with 0.999 it does not."""
+    n = 2 * BLOCK
+    eight, full = make([n], 8, b2=b2, wd=0.0, lr=1e-4), make([n], 32, b2=b2, wd=0.0, lr=1e-4)
+    rng, ref = np.random.default_rng(12), eight[7][0]
+    falls = np.arange(n) % BLOCK >= BLOCK // 2
+    for t in range(3000):
+        g = torch.from_numpy((rng.normal(0, 1e-3, n) * np.where(falls & (t >= 1000), 0.1, 1.0)).astype(np.float32))
+        for made in (eight, full):
+            made[6][0].copy_(g)
+            st.st_adamw_step(made[0])
+        ref.step(g.double().numpy())
+    assert np.array_equal(eight[3][0].cpu().numpy(), ref.cm) and np.array_equal(eight[4][0].cpu().numpy(), ref.cv)
+    assert np.array_equal(eight[5][0][0].cpu().numpy(), ref.ms) and np.array_equal(eight[5][1][0].cpu().numpy(), ref.vs)
+    m, v = [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")]
+    st.st_adamw_read_moments(eight[0], m, v)
+    ratio = np.sqrt(f64(v[0]) / f64(full[4][0]))
+    assert steady[0] <= np.median(ratio[~falls]) <= steady[1] and shrunk[0] <= np.median(ratio[falls]) <= shrunk[1], (np.median(ratio[~falls]), np.median(ratio[falls]))
+    if b2 == 0.99:
+        assert np.all(np.abs(ratio[~falls] - 1) <= 0.07)
+    off, held = f64(m[0]) - f64(full[3][0]), f64(full[3][0])
+    assert np.sqrt(np.mean(off[~falls] ** 2)) <= 0.03 * np.sqrt(np.mean(held[~falls] ** 2))
+    assert torch.isfinite(eight[1][0]).all()
+
+
 @pytest.mark.parametrize("shift", [0, 1])
 def test_levels_next_to_their_borders(shift):
     """Second moments whose root lies on a border between two of the upper levels, or up to four steps of fp32 beside it: the levels are those that the
