@@ -1,8 +1,9 @@
 // st_quantize_rows — rows of activations or weights to 8-bit integers with one scale per row: scale = max |x| / 127, q = x / scale rounded to
 // the nearest whole number (half to even), exactly.
 //
-// Bound by memory: 4 or 2 bytes read and 1 written per value.  Two forms, both reading x once where a row fits registers:
-//   rows whose values lie side by side (tokens, weights): 1 to 8 warps to a row, 16 bytes to an access wherever a row begins
+// Bound by memory: 4 or 2 bytes read and 1 written per value.  Two forms, which read x once where a row fits registers:
+//   rows whose values lie side by side (tokens, weights): 1 to 8 warps to a row, 16 bytes to an access wherever a row begins; rows that are not
+//     aligned are read a second time, from L1
 //   other strides (planar feature maps, whose rows are pixels): a block takes 64 or 128 rows and reads them channel by channel, so that
 //     planes are read 256 bytes at a time; the integers are turned round in shared memory
 //
@@ -170,7 +171,8 @@ __device__ __forceinline__ RowParts parts_of(const T* row, int cols)
 
 // W warps to a row.  ALIGNED: rows of x and q begin where whole pieces can be read and written, and cols is a multiple of V.  Otherwise the integers
 // of a row are gathered in shared memory and written from there in aligned words, whatever the alignment of x's and q's rows.
-// KEEP: a row's pieces stay in registers, kItems of them per lane; otherwise it is read twice, the second time in stretches of that many.
+// KEEP (aligned rows only): a row's pieces stay in registers, kItems of them per lane; otherwise it is read twice, the second time in stretches of
+// that many.
 // Pieces of a lane's stretch, and blocks an SM should hold.  Where pieces go straight to q they stay in registers, and many small blocks are best (8192 x
 // 4096 bf16: 21.0 us with four pieces and six blocks, 24.8 with eight and three).  Rows that go through shared memory are read again from
 // L1 instead (23890 x 3259 fp32: 135 us; 238 with eight pieces in registers and half of the warps).
@@ -179,6 +181,7 @@ template <typename T, int W, bool ALIGNED, bool KEEP>
 __global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 4) quantize_rows_kernel(const T* __restrict__ x, int64_t rows, int cols, int64_t row_stride,
                                                                  int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale)
 {
+    static_assert(ALIGNED || !KEEP, "rows that go through shared memory are read again");
     constexpr int V = Piece<T>::V, kLanes = 32 * W, kItems = ALIGNED ? kItemsStraight : kItemsGathered, kRows = kThreads / kLanes, kStretch = kItems * kLanes;     // pieces
     constexpr int kPitch = kStretch * V + 32;               // bytes of a row's stretch with its head and tail, and what aligning it takes
     __shared__ uint32_t tops[kThreads / 32];
@@ -263,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 6 : 4) quantize_rows_kerne
             for (int i = 0; i < kItems; ++i) {
                 const int at = begin + me + i * kLanes;
                 if (at >= p.pieces) continue;
-                if (!KEEP) get(kept[i], at);
+                get(kept[i], at);
                 uint32_t w[V / 4];
                 pack(w, kept[i]);
                 uint8_t* to = buf + p.head + at * V - first;
@@ -433,17 +436,20 @@ __global__ void plane_scales_kernel(float* scale, int64_t rows)
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 template <typename T>
-cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t cs, int8_t* q, int64_t ldq, float* scale, cudaStream_t s)
+cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t cs, int8_t* q, int64_t ldq, float* scale, int device, cudaStream_t s)
 {
     const bool early = pdl_enabled();
     const int n = (int)cols;
     if (cs != 1 && cols > 1) {
         const int words = aligned(q, 4) && (ldq % 4 == 0 || rows == 1);
         constexpr int per = 32 * 8 / sizeof(T);
-        if (n > kSlab && (rows + per - 1) / per < 74) {         // fewer blocks than half of the SMs
+        int sms = 0;
+        cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+        if (e != cudaSuccess) return e;
+        if (n > kSlab && (rows + per - 1) / per < sms / 2) {    // blocks of whole rows would leave more than half of the SMs idle
             const int groups = (int)((rows + 31) / 32);
             const unsigned grid = (unsigned)(groups * ((cols + kSlab - 1) / kSlab));
-            cudaError_t e = cudaMemsetAsync(scale, 0, sizeof(float) * rows, s);
+            e = cudaMemsetAsync(scale, 0, sizeof(float) * rows, s);
             if (e != cudaSuccess) return e;
             e = launch_early(false, plane_tops_kernel<T>, dim3(grid), dim3(32 * kPlaneWarps), 0, s, x, rows, n, rs, cs, (uint32_t*)scale, groups);
             if (e == cudaSuccess) e = launch_early(false, plane_integers_kernel<T>, dim3(grid), dim3(32 * kPlaneWarps), 0, s, x, rows, n, rs, cs, q, ldq, (const uint32_t*)scale, groups);
@@ -455,7 +461,6 @@ cudaError_t launch(const T* x, int64_t rows, int64_t cols, int64_t rs, int64_t c
         };
         // whole blocks of pixels that lie side by side, then what is left
         const int64_t unit = rs == 1 ? rows / per * per : 0;
-        cudaError_t e = cudaSuccess;
         if (unit) e = n <= kSlab ? go(quantize_planes_kernel<T, true, true>, x, 0, unit) : go(quantize_planes_kernel<T, false, true>, x, 0, unit);
         if (e == cudaSuccess && unit < rows)
             e = n <= kSlab ? go(quantize_planes_kernel<T, true, false>, x + unit * rs, unit, rows - unit) : go(quantize_planes_kernel<T, false, false>, x + unit * rs, unit, rows - unit);
@@ -506,9 +511,9 @@ extern "C" st_status st_quantize_rows(const void* x, int32_t x_type, int64_t row
     b.add("scale", scale, 4, rows, true);
     if (!b.ok()) return b.status();
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    cudaError_t e = x_type == ST_F32 ? launch((const float*)x, rows, cols, row_stride, col_stride, q, ldq, scale, s)
-                  : x_type == ST_BF16 ? launch((const bf16*)x, rows, cols, row_stride, col_stride, q, ldq, scale, s)
-                                      : launch((const __half*)x, rows, cols, row_stride, col_stride, q, ldq, scale, s);
+    cudaError_t e = x_type == ST_F32 ? launch((const float*)x, rows, cols, row_stride, col_stride, q, ldq, scale, b.device(), s)
+                  : x_type == ST_BF16 ? launch((const bf16*)x, rows, cols, row_stride, col_stride, q, ldq, scale, b.device(), s)
+                                      : launch((const __half*)x, rows, cols, row_stride, col_stride, q, ldq, scale, b.device(), s);
     if (e != cudaSuccess) { cudaGetLastError(); return (st_status)fail_on_thread(ST_ERR_CUDA, "st_quantize_rows: %s", cudaGetErrorString(e)); }
     return ST_OK;
 }
