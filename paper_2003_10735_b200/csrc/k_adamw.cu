@@ -186,7 +186,7 @@ __device__ __forceinline__ void decode(float (&m)[kPer], float (&root)[kPer], co
 // itself) and rounded, the one that defines the level from the rounded root (2^-24) and rounded too: 2.5 * 2^-23 between the two, half of it between
 // their roots.  So rounding the approximate root to the nearest whole number gives the level unless it lies next to a border: within 127 * 2^-23 = 1.6e-5
 // of one for m, 255 * 2.25 * 2^-23 = 6.9e-5 for sqrt(v).  There the border, which fp32 holds exactly, decides.
-constexpr float kNearM = 2e-5f, kNearV = 7.5e-5f, kRound = 12582912.f;      // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
+constexpr float kNearM = 2e-5f, kNearV = 7e-5f, kRound = 12582912.f;      // adding 1.5 * 2^23 rounds to a whole number and leaves it in the low bits
 static_assert(kNearM > 127 * 0x1p-23 && kNearV > 255 * 2.25 * 0x1p-23, "values next to a border would not be looked at exactly");
 __device__ __forceinline__ float approximate_root(float r)
 {
@@ -383,7 +383,7 @@ __device__ __forceinline__ void fetch_8(Loads8& l, const TensorRec& t, const voi
     else fetch<true>(l.p, t.param, PARAM, at, kBlockVals, lane);
 }
 // A lane's codes of a block, exactly, from what the block's step reads (old codes and scales, which must not have been overwritten) and the
-// reciprocals of its new scales.  Out of line: a lane in 660 comes here, and its registers are not the step's.
+// reciprocals of its new scales.  Out of line: a lane in 690 comes here, and its registers are not the step's.
 template <int GRAD>
 __device__ __noinline__ uint4 exact_codes(const TensorRec* t, const void* grad, StepNow k, int64_t at, float im, float iv)
 {
@@ -588,24 +588,14 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
 {
     __shared__ double shared[kWarps];
     __shared__ bool last;
-    __shared__ __align__(16) float turned[kWarps][kBlockVals];
     Share share = share_of(p, 0, p.n_chunks, blockIdx.x, gridDim.x);
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     double sum = 0;
-    // Values that were loaded one by one are handed on so that each lane adds the eight that it has on the vector path
     const auto add = [&](const Raw& r, int type, auto vec) {
         float g[kPer];
         convert<decltype(vec)::value>(g, r, type);
-        if (!decltype(vec)::value) {
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) turned[warp][32 * j + lane] = g[j];
-            __syncwarp();
-            const float4 a = *(const float4*)&turned[warp][kPer * lane], b = *(const float4*)&turned[warp][kPer * lane + 4];
-            g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
-        }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) { const double d = g[j]; sum = fma(d, d, sum); }
     };
@@ -625,7 +615,15 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
             }
             for (; at + kBlockVals <= end; at += kChunk) { Raw r; fetch<true>(r, grad, type, at, kBlockVals, lane); add(r, type, std::true_type{}); }
         }
-        for (; at < end; at += kChunk) { Raw r; fetch<false>(r, grad, type, at, (int)min(end - at, (int64_t)kBlockVals), lane); add(r, type, std::false_type{}); }
+        // one by one, each lane the eight values that it has on the vector path
+        for (; at < end; at += kChunk) {
+            const int first = kPer * lane, count = (int)min(end - at, (int64_t)kBlockVals);
+            Raw r;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                r.w[j] = first + j >= count ? 0u : type == ST_F32 ? ((const uint32_t*)grad)[at + first + j] : (uint32_t)((const uint16_t*)grad)[at + first + j];
+            add(r, type, std::false_type{});
+        }
     });
     sum = block_sum(sum, shared);
     if (threadIdx.x == 0) {
