@@ -2,7 +2,7 @@
 // tensors in one launch, moments in fp32 or in 8 bits.  The formulas stand in include/shadowtutor.h.
 //
 // All tensors are cut into chunks of kChunk values; a table on the device says which tensor a chunk belongs to, and each block of a
-// launch that fills the GPU once takes an equal part of them.  A warp takes 256 consecutive values of a chunk, which are also a block of 8-bit
+// launch takes an equal part of them (how many blocks: at st_adamw_create).  A warp takes 256 consecutive values of a chunk, which are also a block of 8-bit
 // moments: the two maxima that a block's scales need are warp reductions, and a lane keeps its eight values in registers from the
 // load to the store, so that every buffer is read once and written once.
 //
@@ -21,7 +21,6 @@
 #include <cstdio>
 #include <new>
 #include <string>
-#include <type_traits>
 #include <vector>
 
 namespace st {
@@ -338,7 +337,7 @@ __device__ __forceinline__ void step_block(const TensorRec& t, int param_type, i
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const float kept = fmaf(-decay, x[j], x[j]);
-        // 8 bits: the quotient to 2^-22 of itself (the arithmetic units bound that form, and its moments are 1 per cent apart)
+        // 8 bits: the quotient to 2^-22 of itself (its moments are levels 1 per cent and more apart)
         const float den = fmaf(root[j], k.r2, k.eps);
         x[j] = fmaf(-lr1, BITS == 32 ? quotient(m[j], den) : __fdividef(m[j], den), kept);
     }
@@ -448,7 +447,7 @@ __device__ __forceinline__ void step_block_8(const TensorRec* record, const Tens
             const f32x2 kept = fma2(decay, xj, xj);
             float d0, d1;
             unpack2(fma2(pack2(root[2 * q], root[2 * q + 1]), r2, eps), d0, d1);
-            // the quotient to 2^-22 of itself: the moments are 1 per cent apart
+            // the quotient to 2^-22 of itself: the moments are levels 1 per cent and more apart
             const f32x2 u = mul2(pack2(m[2 * q], m[2 * q + 1]), pack2(approximate_reciprocal(d0), approximate_reciprocal(d1)));
             unpack2(fma2(lr1, u, kept), x[2 * q], x[2 * q + 1]);
         }
@@ -483,8 +482,8 @@ __device__ __forceinline__ void step_block_8(const TensorRec* record, const Tens
 
 // All whole blocks of a tensor's part; returns where it stopped.  A function of its own for each combination of types: the conversions
 // are decided outside the loop, and the registers are this loop's alone (inlined into the walk, the 8-bit step of 200 M bf16
-// values took 738 us with all combinations side by side and 545 with one compiled alone).  With 8-bit moments, where a warp has much to work out, the next
-// block's loads are on their way meanwhile.
+// values took 738 us with all combinations side by side and 545 with one compiled alone).  A warp loads a block, works it out and stores it; what covers
+// its loads are the other warps of the SM.
 template <int BITS, int PARAM, int GRAD, bool MASTER>
 __device__ __noinline__ int64_t step_blocks(const TensorRec* record, const void* grad, StepNow k, int64_t at, int64_t end)
 {
@@ -593,9 +592,7 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
     pdl_launch_dependents();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     double sum = 0;
-    const auto add = [&](const Raw& r, int type, auto vec) {
-        float g[kPer];
-        convert<decltype(vec)::value>(g, r, type);
+    const auto add = [&](const float (&g)[kPer]) {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) { const double d = g[j]; sum = fma(d, d, sum); }
     };
@@ -611,18 +608,23 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
 #pragma unroll
                 for (int u = 0; u < kFlight; ++u) fetch<true>(r[u], grad, type, at + u * kChunk, kBlockVals, lane);
 #pragma unroll
-                for (int u = 0; u < kFlight; ++u) add(r[u], type, std::true_type{});
+                for (int u = 0; u < kFlight; ++u) { float g[kPer]; convert<true>(g, r[u], type); add(g); }
             }
-            for (; at + kBlockVals <= end; at += kChunk) { Raw r; fetch<true>(r, grad, type, at, kBlockVals, lane); add(r, type, std::true_type{}); }
+            for (; at + kBlockVals <= end; at += kChunk) { Raw r; float g[kPer]; fetch<true>(r, grad, type, at, kBlockVals, lane); convert<true>(g, r, type); add(g); }
         }
         // one by one, each lane the eight values that it has on the vector path
         for (; at < end; at += kChunk) {
-            const int first = kPer * lane, count = (int)min(end - at, (int64_t)kBlockVals);
-            Raw r;
+            const int64_t first = at + kPer * lane;
+            const int count = (int)min(max(end - first, (int64_t)0), (int64_t)kPer);
+            float g[kPer];
+            if (type == ST_F32) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                r.w[j] = first + j >= count ? 0u : type == ST_F32 ? ((const uint32_t*)grad)[at + first + j] : (uint32_t)((const uint16_t*)grad)[at + first + j];
-            add(r, type, std::false_type{});
+                for (int j = 0; j < kPer; ++j) g[j] = j < count ? ((const float*)grad)[first + j] : 0.f;
+            } else {
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) g[j] = from16(j < count ? ((const uint16_t*)grad)[first + j] : 0u, type);
+            }
+            add(g);
         }
     });
     sum = block_sum(sum, shared);
