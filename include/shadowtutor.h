@@ -370,10 +370,10 @@ typedef enum st_dtype { ST_F32 = 0, ST_BF16 = 1, ST_F16 = 2 } st_dtype;
  *     m = c |c| scale, c = -127..127 in int8;     sqrt(v) = c^2 scale, c = 0..255 in uint8
  * where scale is the block's largest |m| / 127^2 (0, with all c = 0, if that |m| is below 2^-100) or its largest sqrt(v) / 255^2.
  * c is the level whose root is nearest: floor(sqrt(|m| / scale) + 1/2); a value with v > 0 has c >= 1, so that no step divides
- * by a second moment that was rounded to nothing.  The levels lie closer together near zero: between 1e-4 of the block's largest
- * value and that value itself they are 1.6 to 16 per cent apart (m; v about half of that in its root).  The step works with the moments in fp32
+ * by a second moment that was rounded to nothing.  Level c lies 2 / c of itself below the next: 1.6 per cent (m) and 0.8 per cent (sqrt(v)) at the block's
+ * largest value, 16 and 8 per cent at 1e-2 of it; at 1e-4 of it the next level is 4 and 2.25 times as large.  The step works with the moments in fp32
  * (with 8 bits: each product and sum rounded by itself, so that equal inputs give equal levels) and parameters see them before they
- * are rounded to levels.  A block that holds a moment that is not finite decodes to values that are not finite or NaN.
+ * are rounded to levels; with 8 bits the update's root and quotient are the device's fast ones, off by up to 2^-21 of the update.  A block that holds a moment that is not finite decodes to values that are not finite or NaN.
  * Levels are rounded to the nearest one after each step, so a moment that changes by less than half the distance of two levels in a step stays where it
  * is.  m forgets a tenth a step (beta1 0.9) and does not come near that: it is 2 per cent off (root of the mean square).  v does with a beta2 near 1:
  *     beta2 up to 0.99    99 of 100 sqrt(v) are within 5 per cent of what fp32 moments hold, however long the run
@@ -494,7 +494,7 @@ ST_API st_status st_quantize_rows(const void *x, int32_t x_type, int64_t rows, i
  * Results depend on the arguments alone, bit for bit.  Returns after enqueueing on cuda_stream (NULL = default stream) and may be
  * captured into a graph; the first call on a device prepares the kernels there and must not be captured.
  * There is no backward: gradients stop at the freeze boundary (Section 4.2), and quantised layers lie in front of it.
- * ST_ERR_INVALID_ARG as for st_quantize_rows; ST_ERR_UNSUPPORTED: K above 131071, more than 2^30 tiles of 128 x 64; ST_ERR_CUDA: also, once, where an
+ * ST_ERR_INVALID_ARG as for st_quantize_rows; ST_ERR_UNSUPPORTED: K above 131071, N above 4194240, more than 2^30 tiles of 128 x 64; ST_ERR_CUDA: also, once, where an
  * earlier product on this stream gave up on a wait and left its result incomplete; this call's product is then enqueued all the same.
  */
 ST_API st_status st_int8_matmul(const int8_t *x, int64_t ldx, const float *x_scale, const int8_t *w, int64_t ldw,

@@ -761,7 +761,8 @@ int launch(const Int8Product& p, unsigned int* err, const Device* d, cudaStream_
     const bool pair = d->sms >= 2 && time_of(2 * kTile, 256, d->sms / 2, 0.30, 2.3) < tiles_time(bn);
     const int bt = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
     const int64_t n_split_tiles = (p.N + kTile - 1) / kTile;
-    // As many blocks to a tile as the SMs allow (a few more blocks than SMs are let in: two of them fit one), with two slices of K each at least
+    // As many blocks to a tile as the SMs allow, with a slice of K each at least.  A few more blocks than SMs are let in: where a block's stages take
+    // less than half of an SM's shared memory two fit one, otherwise (128 tokens x 4096 x 2560: 160 blocks of 128 KB) the last clusters wait for the first
     int splits = 1;
     while (splits < kMaxSplits && n_split_tiles * splits * 2 <= d->sms + 20 && slices >= splits * 2) splits *= 2;
     const double weight_time = (double)p.N * (double)p.K / 5.5e6, slice_time = 0.16 * ((slices + splits - 1) / splits) * (double)((n_split_tiles * splits + d->sms - 1) / d->sms);
