@@ -495,7 +495,8 @@ ST_API st_status st_quantize_rows(const void *x, int32_t x_type, int64_t rows, i
  * captured into a graph; the first call on a device prepares the kernels there and must not be captured.
  * There is no backward: gradients stop at the freeze boundary (Section 4.2), and quantised layers lie in front of it.
  * ST_ERR_INVALID_ARG as for st_quantize_rows; ST_ERR_UNSUPPORTED: K above 131071, N above 4194240, more than 2^30 tiles of 128 x 64; ST_ERR_CUDA: also, once, where an
- * earlier product on this stream gave up on a wait and left its result incomplete; this call's product is then enqueued all the same.
+ * earlier product on this stream, or one of a replayed graph on this device, gave up on a wait and left its result incomplete; this call's product is
+ * then enqueued all the same.
  */
 ST_API st_status st_int8_matmul(const int8_t *x, int64_t ldx, const float *x_scale, const int8_t *w, int64_t ldw,
                                 const float *w_scale, const float *bias, int32_t relu, int64_t M, int64_t N, int64_t K,

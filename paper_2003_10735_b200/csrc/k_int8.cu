@@ -686,7 +686,9 @@ __global__ void __launch_bounds__(256) int8_plain_kernel(const int8_t* __restric
 // ---- host ------------------------------------------------------------------------------------------------------------
 // What a device needs before its first launch: the kernels' limits of shared memory, and words in pinned host memory in which a wait that gave up
 // leaves its code, so that the next call on the same stream can tell without waiting for the device.  Streams, by their handles, have words of their
-// own, up to kErrWords of them; any more share.  (Their numbers, cudaStreamGetId, cannot be asked for while they are captured.)
+// own, up to kErrWords of them; any more share.  (Their numbers, cudaStreamGetId, cannot be asked for while they are captured.)  One more word is for
+// launches that become part of a graph: it may be replayed on any stream, and the one that was captured may see no call again, so that whichever
+// call comes next tells of them.
 constexpr int kMaxDevices = 64, kErrWords = 1024;
 struct Device { bool ready = false; int sms = 0; unsigned int *err = nullptr, *err_dev = nullptr; uintptr_t owner[kErrWords] = {}; };
 Device g_devices[kMaxDevices];
@@ -709,8 +711,8 @@ cudaError_t device_for(int index, cudaStream_t s, Device** out, int* word)
     for (const void* k : {(const void*)int8_tiles_kernel<64>, (const void*)int8_tiles_kernel<128>, (const void*)int8_tiles_kernel<256>, (const void*)int8_pair_kernel,
                           (const void*)int8_split_kernel<16>, (const void*)int8_split_kernel<32>, (const void*)int8_split_kernel<64>, (const void*)int8_split_kernel<128>})
         if (e == cudaSuccess) e = allow_shared_memory(k);
-    if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, kErrWords * sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
-    if (e == cudaSuccess) { std::fill_n(d.err, kErrWords, 0u); e = cudaHostGetDevicePointer((void**)&d.err_dev, d.err, 0); }
+    if (e == cudaSuccess && !d.err) e = cudaHostAlloc((void**)&d.err, (kErrWords + 1) * sizeof(unsigned int), cudaHostAllocMapped | cudaHostAllocPortable);
+    if (e == cudaSuccess) { std::fill_n(d.err, kErrWords + 1, 0u); e = cudaHostGetDevicePointer((void**)&d.err_dev, d.err, 0); }
     d.ready = e == cudaSuccess;
     return e;
 }
@@ -874,15 +876,15 @@ int int8_matmul(const Int8Product& p, cudaStream_t s)
     const cudaError_t e = device_for(b.device(), s, &d, &word);
     if (e != cudaSuccess) return cuda_fail(e);
     if (p.err) return launch(p, p.err, d, s);
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) { cudaGetLastError(); capture = cudaStreamCaptureStatusNone; }
+    const int status = launch(p, d->err_dev + (capture == cudaStreamCaptureStatusNone ? word : kErrWords), d, s);
+    if (status != ST_OK) return status;
     // what an earlier product has left is told once, and this product is enqueued all the same: what gave up need not be the caller's
-    const unsigned int code = __atomic_exchange_n(d->err + word, 0u, __ATOMIC_RELAXED);
-    const int status = launch(p, d->err_dev + word, d, s);
-    if (status != ST_OK) {
-        unsigned int none = 0;
-        if (code) __atomic_compare_exchange_n(d->err + word, &none, code, false, __ATOMIC_RELAXED, __ATOMIC_RELAXED);
-        return status;
-    }
-    if (code) return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of an earlier product on this stream gave up (code %u); its result is not complete", code);
+    if (const unsigned int code = __atomic_exchange_n(d->err + word, 0u, __ATOMIC_RELAXED))
+        return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of a product on this stream gave up (code %u); its result is not complete", code);
+    if (const unsigned int code = __atomic_exchange_n(d->err + kErrWords, 0u, __ATOMIC_RELAXED))
+        return fail_on_thread(ST_ERR_CUDA, "st_int8_matmul: a device wait of a product in a replayed graph gave up (code %u); its result is not complete", code);
     return ST_OK;
 }
 

@@ -356,6 +356,30 @@ def test_a_product_that_gave_up_is_told_of_on_its_own_stream(monkeypatch):
     st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())
 
 
+def test_a_product_that_gave_up_inside_a_graph_is_told_of_by_the_next_call(monkeypatch):
+    """The stream that was captured may see no call again: whichever product comes next on the device tells of it, once, and is there itself."""
+    m, n, k = 40, 200, 1024
+    x, w, sx, sw = matrix(m, k, 0), matrix(n, k, 1), torch.rand(m, device="cuda"), torch.rand(n, device="cuda")
+    ys = [torch.zeros(m, n, device="cuda") for _ in range(3)]
+    st.st_int8_matmul(x, sx, w, sw, ys[0], cuda_stream=stream())
+    torch.cuda.synchronize()
+    monkeypatch.setenv("ST_TEST_STALL_INT8", "1")
+    graph, captured = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=captured, capture_error_mode="thread_local"):
+        st.st_int8_matmul(x, sx, w, sw, ys[1], cuda_stream=torch.cuda.current_stream().cuda_stream)
+    monkeypatch.delenv("ST_TEST_STALL_INT8")
+    st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())            # nothing has run yet
+    graph.replay()
+    torch.cuda.synchronize()
+    ys[2].zero_()
+    with pytest.raises(st.StError) as ei:
+        st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())
+    assert ei.value.status == st.ST_ERR_CUDA and "graph gave up" in str(ei.value)
+    torch.cuda.synchronize()
+    assert torch.equal(ys[2].cpu(), ref_matmul(x, sx, w, sw, None, False, "f32"))
+    st.st_int8_matmul(x, sx, w, sw, ys[2], cuda_stream=stream())
+
+
 @pytest.mark.parametrize("k,n", [(96, 48), (97, 33)])
 def test_matrices_that_lie_beside_each_other_in_one_buffer(k, n):
     """Integers behind the rows that they are made from, products behind the integers: no byte is shared, and nothing else changes."""
