@@ -618,8 +618,17 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
             const int count = (int)min(max(end - first, (int64_t)0), (int64_t)kPer);
             float g[kPer];
             if (type == ST_F32) {
+                const float* q = (const float*)grad + first;
+                if (count == kPer) {                    // in pairs where they lie at multiples of 8 bytes: half of the accesses
+                    const bool odd = (uintptr_t)q & 4;
+                    if (odd) { g[0] = q[0]; g[7] = q[7]; ++q; }
+                    const float2 a = *(const float2*)q, b = *(const float2*)(q + 2), c = *(const float2*)(q + 4);
+                    if (odd) { g[1] = a.x; g[2] = a.y; g[3] = b.x; g[4] = b.y; g[5] = c.x; g[6] = c.y; }
+                    else { const float2 d = *(const float2*)(q + 6); g[0] = a.x; g[1] = a.y; g[2] = b.x; g[3] = b.y; g[4] = c.x; g[5] = c.y; g[6] = d.x; g[7] = d.y; }
+                } else {
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) g[j] = j < count ? ((const float*)grad)[first + j] : 0.f;
+                    for (int j = 0; j < kPer; ++j) g[j] = j < count ? q[j] : 0.f;
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) g[j] = from16(j < count ? ((const uint16_t*)grad)[first + j] : 0u, type);
